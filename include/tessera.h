@@ -4,7 +4,8 @@
  * The path is the per-layer GPU work of a prompt whose context units already
  * have cached KV (Sec. 5.3 of the paper, "Coordinated Request Execution"):
  *
- *   placement  -> tessera_plan_create          (host, once per batch)
+ *   placement  -> tessera_plan_create          (host, once per batch; tessera_plan_create_windowed
+ *                                               for layers with a sliding window)
  *   gather     -> tessera_kv_compose           (device, per layer)
  *   RoPE shift -> tessera_rope_shift           (device, per layer; normally fused into compose)
  *   attention  -> tessera_partial_prefill_attn (device, per layer)
@@ -157,6 +158,20 @@ typedef struct tessera_plan_info {
  */
 TESSERA_API int32_t tessera_plan_create(const tessera_model_cfg *cfg, const tessera_compose_desc *desc,
                             int32_t num_pool_pages, uint32_t flags, tessera_plan **out, void *stream);
+
+/*
+ * The same for a layer with a SLIDING WINDOW whose first tokens stay visible (sinks).  (The paper's models
+ * attend to everything; this is for those that do not.)  Every attention call of the plan - 16-bit and
+ * 8-bit keys, the host entry points - lets a query at position p see the keys k <= p with k < n_sink or
+ * k > p - window, i.e. the last `window` positions up to its own and the first n_sink.  Keys that no query
+ * of the batch sees are never read as numbers (their pages may hold anything, NaN included) and most of
+ * their pages not at all.  plan_info counts visible pairs.
+ *   window: 0 = no window (n_sink is then ignored, and the call is tessera_plan_create); n_sink >= 0.
+ *           Negative values are TESSERA_INVALID_ARG.
+ */
+TESSERA_API int32_t tessera_plan_create_windowed(const tessera_model_cfg *cfg, const tessera_compose_desc *desc,
+                                     int32_t num_pool_pages, int32_t window, int32_t n_sink, uint32_t flags,
+                                     tessera_plan **out, void *stream);
 
 /* Frees the plan (device memory may be kept for later plans).  The caller must have synchronised every stream that used the plan. */
 TESSERA_API int32_t tessera_plan_destroy(tessera_plan *plan);

@@ -54,7 +54,7 @@ class PlanInfo(ctypes.Structure):
                 ("retained_tokens", ctypes.c_int64), ("attn_mma_pairs", ctypes.c_int64)]
 
 
-EXPORTS = ["tessera_plan_create", "tessera_plan_destroy", "tessera_plan_block_table", "tessera_plan_get_info",
+EXPORTS = ["tessera_plan_create", "tessera_plan_create_windowed", "tessera_plan_destroy", "tessera_plan_block_table", "tessera_plan_get_info",
            "tessera_plan_status", "tessera_kv_compose", "tessera_kv_compose_from", "tessera_kv_compose_from_fp8", "tessera_kv_retain_fp8", "tessera_rope_shift", "tessera_rope_fresh", "tessera_extend_write", "tessera_partial_prefill_attn", "tessera_kv_compose_k8", "tessera_partial_prefill_attn_k8",
            "tessera_composed_prefill_host", "tessera_composed_prefill_host_tier", "tessera_rope_shift_static", "tessera_selftest_bounded_wait", "tessera_last_error",
            "tessera_launch_count"]
@@ -62,6 +62,8 @@ EXPORTS = ["tessera_plan_create", "tessera_plan_destroy", "tessera_plan_block_ta
 _vp = ctypes.c_void_p
 _lib.tessera_plan_create.argtypes = [ctypes.POINTER(ModelCfg), ctypes.POINTER(ComposeDesc), ctypes.c_int32,
                                      ctypes.c_uint32, ctypes.POINTER(_vp), _vp]
+_lib.tessera_plan_create_windowed.argtypes = [ctypes.POINTER(ModelCfg), ctypes.POINTER(ComposeDesc), ctypes.c_int32,
+                                              ctypes.c_int32, ctypes.c_int32, ctypes.c_uint32, ctypes.POINTER(_vp), _vp]
 _lib.tessera_plan_destroy.argtypes = [_vp]
 _lib.tessera_plan_block_table.argtypes = [_vp, ctypes.POINTER(_I32P), ctypes.POINTER(_I32P), ctypes.POINTER(_I32P)]
 _lib.tessera_plan_get_info.argtypes = [_vp, ctypes.POINTER(PlanInfo)]
@@ -134,9 +136,10 @@ def _stream(stream) -> Optional[int]:
 
 class Plan:
     """tessera_plan_create / tessera_plan_destroy with host arrays taken from a Workload-like
-    object (anything with the descriptor's field names and a `.shape` model description)."""
+    object (anything with the descriptor's field names and a `.shape` model description).  With `window` > 0
+    its attention calls see the last `window` positions and the first `n_sink` (tessera_plan_create_windowed)."""
 
-    def __init__(self, w, host_only: bool = False, stream=None, inv_freq=None):
+    def __init__(self, w, host_only: bool = False, stream=None, inv_freq=None, window: int = 0, n_sink: int = 0):
         sh = w.shape
         self._keep = [_arr(getattr(w, f)) for f in
                       ("seq_len", "unit_off", "unit_len", "unit_cached_pos", "unit_cached_stride",
@@ -156,9 +159,11 @@ class Plan:
         self._opt = opt
         self._h = _vp()
         self.host_only = host_only
-        st = _lib.tessera_plan_create(ctypes.byref(cfg), ctypes.byref(desc), int(w.num_pool_pages),
-                                      PLAN_HOST_ONLY if host_only else 0, ctypes.byref(self._h),
-                                      None if host_only else _stream(stream))
+        args = (PLAN_HOST_ONLY if host_only else 0, ctypes.byref(self._h), None if host_only else _stream(stream))
+        if window == 0 and n_sink == 0:
+            st = _lib.tessera_plan_create(ctypes.byref(cfg), ctypes.byref(desc), int(w.num_pool_pages), *args)
+        else:
+            st = _lib.tessera_plan_create_windowed(ctypes.byref(cfg), ctypes.byref(desc), int(w.num_pool_pages), int(window), int(n_sink), *args)
         _check(st)
         self.batch = len(a[0])
         self.info = PlanInfo()

@@ -185,6 +185,11 @@ extern "C" {
 
 int32_t tessera_plan_create(const tessera_model_cfg *cfg, const tessera_compose_desc *desc, int32_t num_pool_pages,
                             uint32_t flags, tessera_plan **out, void *stream) {
+    return tessera_plan_create_windowed(cfg, desc, num_pool_pages, 0, 0, flags, out, stream);
+}
+
+int32_t tessera_plan_create_windowed(const tessera_model_cfg *cfg, const tessera_compose_desc *desc, int32_t num_pool_pages,
+                                     int32_t window, int32_t n_sink, uint32_t flags, tessera_plan **out, void *stream) {
     if (!out) return set_error(TESSERA_INVALID_ARG, "null out pointer");
     *out = nullptr;
     if (flags & ~uint32_t(TESSERA_PLAN_HOST_ONLY)) return set_error(TESSERA_INVALID_ARG, "unknown plan flag");
@@ -200,7 +205,7 @@ int32_t tessera_plan_create(const tessera_model_cfg *cfg, const tessera_compose_
         if (!pl) return set_error(TESSERA_INVALID_ARG, "out of host memory");
         bool no_memory = false;
         try {
-            st = build_plan_host(cfg, desc, num_pool_pages, num_sms, cut, pl, &err);
+            st = build_plan_host(cfg, desc, num_pool_pages, num_sms, cut, pl, &err, window, n_sink);
             if (st != TESSERA_OK) set_error(st, err);
             pl->host_only = host_only;
             if (st == TESSERA_OK && !host_only) st = upload(pl, static_cast<cudaStream_t>(stream), &no_memory);

@@ -128,7 +128,9 @@ struct FirstItem {
 // K8: queries and keys are 8-bit floats (e4m3 codes; the scales are folded into scale_log2 by the host):
 // S = Q K^T runs as kind::f8f6f4 with 32 elements of head_dim per instruction, a Q tile and a K step are
 // 128 rows of 128 bytes (one swizzle atom wide, head_dim 128 only); V, P and the accumulator stay as they are.
-template <int D, int kMaxPages, bool K8>
+// W: a query at p sees the keys k <= p with k < n_sink or k > p - window.  The work list leaves out the steps that no row
+// of an item sees (AttnWork::sink_steps, gap), so all the kernel adds is the lower limit in the steps it falls in.
+template <int D, int kMaxPages, bool K8, bool W>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CUtensorMap tmap_o,
@@ -136,7 +138,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                const AttnWork *__restrict__ work, int n_work, const int32_t *__restrict__ q_pos,
                const int32_t *__restrict__ pages, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse,
                int H_q, int g, int page_size, int num_pool_pages, float scale_log2,
-               float *__restrict__ ws_o, float2 *__restrict__ ws_ml, int *status) {
+               float *__restrict__ ws_o, float2 *__restrict__ ws_ml, int *status, int window, int n_sink) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     using G = Geo<D>;
@@ -177,13 +179,20 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
         // the item covers the 128-key steps [step0, step_end) of its tiles (all of them unless it was
         // split); step indices below are relative to step0
         it.step0 = it.wk.step_begin;
-        it.n_steps0 = min(it.wk.step_end, (it.t0.kv_len + kStep - 1) / kStep) - it.step0;
-        it.n_steps1 = it.n_tiles == 2 ? min(it.wk.step_end, (it.t1.kv_len + kStep - 1) / kStep) - it.step0 : 0;
+        it.n_steps0 = min(it.wk.step_end, (it.t0.kv_len + kStep - 1) / kStep - (W ? it.wk.gap : 0)) - it.step0;
+        it.n_steps1 = it.n_tiles == 2 ? min(it.wk.step_end, (it.t1.kv_len + kStep - 1) / kStep - (W ? it.wk.gap : 0)) - it.step0 : 0;
         it.n_steps = max(it.n_steps0, it.n_steps1);
         it.T = it.wk.seq_len;
         it.req_pages = (it.T + page_size - 1) / page_size;
         it.bt = pages + it.wk.page_begin;
         return it;
+    };
+    // the 128-key step of the request that step v of the item's count is
+    auto real_step = [](const Item &it, int v) { return W && v >= it.wk.sink_steps ? v + it.wk.gap : v; };
+    // block-table index of the page that lane `lane` brings of the steps from v on (32 pages)
+    auto page_index = [&](const Item &it, int v) {
+        if constexpr (W) return pps * real_step(it, v + lane / pps) + lane % pps;
+        else return pps * v + lane;
     };
 
     if (tid == 0) {
@@ -221,7 +230,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                 s_first.t[0] = it.t0;
                 s_first.t[1] = it.t1;
             }
-            const int pi = pps * it.step0 + lane;
+            const int pi = page_index(it, it.step0);
             s_first.page[lane] = pi < it.req_pages ? it.bt[pi] : num_pool_pages;
         }
     }
@@ -290,7 +299,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
             for (int j0 = 0; j0 < it.n_steps; j0 += steps_per_fetch) {
                 // lane l holds the id of page (pps * (step0 + j0) + l); a page past the request's last one
                 // is fetched from outside the pool, which TMA fills with zeros
-                const int pi = pps * (it.step0 + j0) + lane;
+                const int pi = page_index(it, it.step0 + j0);
                 const int my_page = round == 0 && j0 == 0 ? s_first.page[lane] : pi < it.req_pages ? it.bt[pi] : num_pool_pages;
                 const int jn = min(steps_per_fetch, it.n_steps - j0);
                 for (int jj = 0; jj < jn; ++jj) {
@@ -339,7 +348,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
             const int n_steps = it.n_steps;
             const int my_steps = q ? it.n_steps1 : it.n_steps0;
             const int T = it.T, step0 = it.step0;
-            const int tail_step = (T % kStep) ? T / kStep - step0 : -1;   // step holding slots past the sequence end
+            const int tail_step = (T % kStep) ? T / kStep - step0 - (W ? it.wk.gap : 0) : -1;   // step holding slots past the sequence end
 
             auto ring_wait = [&](int item, int code) {
                 item += ring_base;
@@ -393,7 +402,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                     __syncwarp();
                     continue;
                 }
-                if (j == tail_step) {
+                if (!W && j == tail_step) {          // (with a window: below)
                     // V rows past the end of the sequence hold whatever the page held before; their
                     // probabilities are zero, but 0 x NaN would still poison the accumulator.  (Both
                     // issuing warps may write these zeros; the values agree.)
@@ -410,6 +419,22 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                     }
                     fence_proxy_async_smem();
                     __syncwarp();
+                }
+                if constexpr (W) {
+                    // V rows between the sinks and the window of the item's first row, and behind its last row: no row of the item
+                    // sees them, and they may hold anything too (pages that have left the window are free to be given away)
+                    const int key0 = real_step(it, step0 + j) * kStep;
+                    const int kv_end = it.n_tiles == 2 ? it.t1.kv_len : it.t0.kv_len;
+                    const int r0 = max(n_sink - key0, 0), r1 = min(it.t0.kv_full - window - key0, kStep), r2 = kv_end - key0;
+                    if (r0 < r1 || r2 < kStep) {
+                        uint8_t *v = sm + kSmemRing + vslot * kSlotBytes;
+                        for (int r = lane >> 3; r < kStep; r += 4)
+                            if ((r >= r0 && r < r1) || r >= r2)
+#pragma unroll
+                                for (int hf = 0; hf < G::kHalves; ++hf) *reinterpret_cast<uint4 *>(v + hf * kHalfBytes + r * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
                 }
                 const bool next_s = j + 1 < my_steps;
                 if (more) ring_wait(2 * j + 2, 3);                     // K_{j+1}
@@ -501,8 +526,9 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                 // S_j complete; this also means P.V of step j-1 has completed (it was issued earlier)
                 mbar_wait(smem_u32(&bars.s_full[q]), par, abort_flag, status, 7);
                 tc_fence_after();
-                const int key0 = (step0 + j) * kStep;
-                const bool masked = key0 + kStep > (q ? t1.kv_full : t0.kv_full);   // a causal limit falls in this step
+                const int key0 = real_step(it, step0 + j) * kStep;
+                bool masked = key0 + kStep > (q ? t1.kv_full : t0.kv_full);   // a causal limit falls in this step
+                if constexpr (W) masked = masked || (key0 < (q ? t1.kv_len : t0.kv_len) - window && key0 + kStep > n_sink);   // or a window's
 
                 // The thread's 2 x 64 scores (rows t/4 and t/4 + 8 of the warp's 16; of every group of 8
                 // columns, columns 2 (t%4) and 2 (t%4) + 1) stay in registers for the whole step.
@@ -514,7 +540,10 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                     for (int k = 0; k < 16; ++k)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (key0 + 8 * k + cq + (e & 1) > p_row[q][e >> 1]) s[4 * k + e] = 0xff800000u;   // -inf
+                        {
+                            const int key = key0 + 8 * k + cq + (e & 1), p = p_row[q][e >> 1];
+                            if (key > p || (W && key >= n_sink && key <= p - window)) s[4 * k + e] = 0xff800000u;   // -inf
+                        }
                 }
                 uint32_t pk[16];
                 // Probabilities of column groups [8 h, 8 h + 8) (keys [64 h, 64 h + 64)) against the current
@@ -585,6 +614,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                 // second half (the first half's P.V is brought to the new reference with the accumulator).
                 float sum_a[2], sum_b[2], factor[2];
                 bool fresh = j == 0;
+                // (a row whose first keys are still to come has no reference yet: the one it starts with may be far off)
+                if constexpr (W) fresh = fresh || __any_sync(0xffffffffu, m_row[q][0] == -INFINITY || m_row[q][1] == -INFINITY);
                 if (!fresh) {
                     exp_half(0, sum_a);
                     fresh = __any_sync(0xffffffffu, !(sum_a[0] <= 64.f && sum_a[1] <= 64.f));
@@ -795,7 +826,7 @@ attn_combine_kernel(const CombineItem *__restrict__ items, const float *__restri
     }
 }
 
-template <int D, int kMaxPages, bool K8>
+template <int D, int kMaxPages, bool K8, bool W>
 cudaError_t launch_attn_tc_d(const tessera_plan *pl, void *k_pool, void *v_pool, const void *q, void *out,
                              float *lse, int chunk, int max_blocks, float qk_scale, cudaStream_t st, std::string *err) {
     const AttnWork *work = chunk < 0 ? pl->dev.work : pl->dev.work_chunked + pl->chunk_work_off[chunk];
@@ -817,7 +848,7 @@ cudaError_t launch_attn_tc_d(const tessera_plan *pl, void *k_pool, void *v_pool,
     }
     if (!make_q_tmap(&to, out, pl->n_q, Hq, D, g, kRows / g, err)) return cudaErrorInvalidValue;   // `out` has the layout of a 16-bit q
     if (!make_pool_tmap(&tv, v_pool, pl->num_pool_pages, ps, Hkv, D, err)) return cudaErrorInvalidValue;
-    cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, kMaxPages, K8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Geo<D>::kSmemAlloc);
+    cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, kMaxPages, K8, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Geo<D>::kSmemAlloc);
     if (e != cudaSuccess) { *err = "cudaFuncSetAttribute(shared memory)"; return e; }
     const DeviceTables &d = pl->dev;
     const float scale_log2 = pl->sm_scale * 1.4426950408889634f * qk_scale;
@@ -829,8 +860,8 @@ cudaError_t launch_attn_tc_d(const tessera_plan *pl, void *k_pool, void *v_pool,
     const bool chained = pl->chained && chunk < 0;
     if (chained && grid % 2 != 0 && max_blocks <= 0 && grid < (unsigned)pl->num_sms) ++grid;      // (a block without an item ends at once)
     e = launch_clusters(
-        attn_tc_kernel<D, kMaxPages, K8>, grid, kThreads, chained && grid % 2 == 0 ? 2 : 1, Geo<D>::kSmemAlloc, st, chained, tq, tk, tv, to, d.tiles, work, (int)n_work, d.q_pos, d.pages,
-        static_cast<__nv_bfloat16 *>(out), lse, Hq, g, ps, pl->num_pool_pages, scale_log2, d.ws_o, d.ws_ml, d.status);
+        attn_tc_kernel<D, kMaxPages, K8, W>, grid, kThreads, chained && grid % 2 == 0 ? 2 : 1, Geo<D>::kSmemAlloc, st, chained, tq, tk, tv, to, d.tiles, work, (int)n_work, d.q_pos, d.pages,
+        static_cast<__nv_bfloat16 *>(out), lse, Hq, g, ps, pl->num_pool_pages, scale_log2, d.ws_o, d.ws_ml, d.status, pl->window, pl->n_sink);
     if (e == cudaSuccess && !pl->combine.empty()) {
         const int c0 = chunk < 0 ? 0 : pl->chunk_combine_off[chunk];
         const int c1 = chunk < 0 ? (int)pl->combine.size() : pl->chunk_combine_off[chunk + 1];
@@ -852,11 +883,12 @@ cudaError_t launch_attn_tc(const tessera_plan *pl, void *k_pool, void *v_pool, c
         *err = "shape outside the tcgen05 kernel's range";
         return cudaErrorNotSupported;
     }
-    if (ps == 8)
-        return D == 128 ? launch_attn_tc_d<128, 16, false>(pl, k_pool, v_pool, q, out, lse, chunk, max_blocks, 1.f, st, err)
-                        : launch_attn_tc_d<64, 16, false>(pl, k_pool, v_pool, q, out, lse, chunk, max_blocks, 1.f, st, err);
-    return D == 128 ? launch_attn_tc_d<128, 8, false>(pl, k_pool, v_pool, q, out, lse, chunk, max_blocks, 1.f, st, err)
-                    : launch_attn_tc_d<64, 8, false>(pl, k_pool, v_pool, q, out, lse, chunk, max_blocks, 1.f, st, err);
+    const bool w = pl->window > 0;
+    auto launch = D == 128 ? (ps == 8 ? (w ? launch_attn_tc_d<128, 16, false, true> : launch_attn_tc_d<128, 16, false, false>)
+                                      : (w ? launch_attn_tc_d<128, 8, false, true> : launch_attn_tc_d<128, 8, false, false>))
+                           : (ps == 8 ? (w ? launch_attn_tc_d<64, 16, false, true> : launch_attn_tc_d<64, 16, false, false>)
+                                      : (w ? launch_attn_tc_d<64, 8, false, true> : launch_attn_tc_d<64, 8, false, false>));
+    return launch(pl, k_pool, v_pool, q, out, lse, chunk, max_blocks, 1.f, st, err);
 }
 
 cudaError_t launch_attn_tc_k8(const tessera_plan *pl, void *k_pool8, void *v_pool, const void *q8, void *out,
@@ -867,8 +899,10 @@ cudaError_t launch_attn_tc_k8(const tessera_plan *pl, void *k_pool8, void *v_poo
         *err = "8-bit keys: head_dim 128 only";
         return cudaErrorNotSupported;
     }
-    return ps == 8 ? launch_attn_tc_d<128, 16, true>(pl, k_pool8, v_pool, q8, out, lse, -1, 0, qk_scale, st, err)
-                   : launch_attn_tc_d<128, 8, true>(pl, k_pool8, v_pool, q8, out, lse, -1, 0, qk_scale, st, err);
+    const bool w = pl->window > 0;
+    auto launch = ps == 8 ? (w ? launch_attn_tc_d<128, 16, true, true> : launch_attn_tc_d<128, 16, true, false>)
+                          : (w ? launch_attn_tc_d<128, 8, true, true> : launch_attn_tc_d<128, 8, true, false>);
+    return launch(pl, k_pool8, v_pool, q8, out, lse, -1, 0, qk_scale, st, err);
 }
 
 }  // namespace tessera

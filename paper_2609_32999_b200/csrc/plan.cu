@@ -31,11 +31,16 @@ bool is_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 }  // namespace
 
 int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc *d,
-                        int32_t num_pool_pages, int num_sms, bool may_cut, tessera_plan *pl, std::string *err) {
+                        int32_t num_pool_pages, int num_sms, bool may_cut, tessera_plan *pl, std::string *err, int32_t window, int32_t n_sink) {
     auto fail = [&](int32_t code, const std::string &msg) { *err = msg; return code; };
     if (!cfg || !d || !pl) return fail(TESSERA_INVALID_ARG, "null cfg / desc / plan");
     if (num_sms <= 0) return fail(TESSERA_INVALID_ARG, "multiprocessor count must be positive");
     pl->num_sms = num_sms;
+    if (window < 0 || n_sink < 0) return fail(TESSERA_INVALID_ARG, "negative window or sink count");
+    window = std::min(window, 1 << 30);        // (more than any pool holds; sums and differences of it and a position stay in 32 bits)
+    n_sink = window > 0 ? std::min(n_sink, 1 << 30) : 0;
+    pl->window = window;
+    pl->n_sink = n_sink;
     if (d->batch < 0 || num_pool_pages < 0 || d->n_free < 0)
         return fail(TESSERA_INVALID_ARG, "negative batch, pool size or free-list length");
     if (d->batch > 0 && (!d->seq_len || !d->unit_off || !d->recompute_off))
@@ -202,7 +207,8 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
             fresh[base + p] = 1;
             fresh_row[base + p] = j;
             pl->fresh_dst[j] = pl->pages[pl->page_off[r] + p / B] * B + p % B;
-            pl->qk_pairs += (int64_t)p + 1;
+            pl->qk_pairs += window > 0 ? std::min((int64_t)p + 1, (int64_t)window + std::min((int64_t)n_sink, std::max((int64_t)p + 1 - window, (int64_t)0)))
+                                       : (int64_t)p + 1;
         }
         for (int p = 0; p < T; ++p)
             if (pl->src_slot[base + p] < 0 && !fresh[base + p])
@@ -335,8 +341,14 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
     pl->attn_kernel = 1;       // the tcgen05 kernel covers every accepted shape (page size 8..128, head_dim 64 / 128, g <= 16)
     pl->tiles.clear();
     for (int r = 0; r < batch; ++r)
-        for (int j0 = d->recompute_off[r]; j0 < d->recompute_off[r + 1]; j0 += pl->tile_tokens) {
-            const int n = std::min(pl->tile_tokens, d->recompute_off[r + 1] - j0);
+        for (int j0 = d->recompute_off[r], n; j0 < d->recompute_off[r + 1]; j0 += n) {
+            n = std::min(pl->tile_tokens, d->recompute_off[r + 1] - j0);
+            // With a window a tile ends where the next row's window leaves keys out behind the row before: the keys between a
+            // tile's first and last are then all some row's, so none is read for nothing and none that nobody sees gets
+            // into a product.  (Runs of 16 rows every 512, window 128: modelled 11 200 cycles a run, 10 400 in tiles of two.)
+            if (window > 0)
+                for (int i = 1; i < n; ++i)
+                    if (d->recompute_pos[j0 + i] - window > d->recompute_pos[j0 + i - 1]) n = i;
             AttnTile t{};
             t.req = r; t.q_begin = j0; t.n_tok = n;
             t.kv_len = d->recompute_pos[j0 + n - 1] + 1;
@@ -349,17 +361,14 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
     {
         const int page = 128;        // keys per step of the tensor-core kernel
         std::vector<std::pair<int32_t, int32_t>> pairs;
-        size_t first = 0;
-        while (first < pl->tiles.size()) {
-            size_t last = first;
-            while (last < pl->tiles.size() && pl->tiles[last].req == pl->tiles[first].req) ++last;
-            for (size_t k = first; k < last; k += 2) {
-                const int32_t a = (int32_t)k, b2 = (k + 1 < last) ? (int32_t)(k + 1) : -1;
-                pairs.push_back({a, b2});
-            }
-            first = last;
-        }
-        auto steps_of = [&](int32_t tile) { return (pl->tiles[tile].kv_len + page - 1) / page; };
+        // With a window an item leaves out the steps between its sinks and the window of its first row: gap[tile] of them.
+        // (Where the window begins in the sinks' last step or before, there are none.)
+        const int sink_steps = window > 0 ? (int)(((int64_t)pl->n_sink + page - 1) / page) : 0;
+        std::vector<int32_t> gap(pl->tiles.size(), 0);
+        auto gap_at = [&](int32_t tile) {
+            return window > 0 ? std::max(0, std::max(0, pl->tiles[tile].kv_full - window) / page - sink_steps) : 0;
+        };
+        auto steps_of = [&](int32_t tile) { return (pl->tiles[tile].kv_len + page - 1) / page - gap[tile]; };
         // Modelled cycles of an item (clock64 on a B200): item fetch 1 700, epilogue and what the first step takes
         // longer than a later one 4 700 per tile, 3 180 per step of both tiles, 2 400 per step of a lone one (whose
         // softmax and MMAs wait for each other).
@@ -367,6 +376,21 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
             const int both = std::min(steps_a, steps_b), single = std::max(steps_a, steps_b) - both;
             return 1700 + (int64_t)n_tiles * 4700 + (int64_t)both * 3180 + (int64_t)single * 2400;
         };
+        // Consecutive tiles of a request pair up.  With a window they do where the model gives the pair no more cycles than
+        // two items: tile b also walks the steps that only tile a sees, which rows scattered over a long prompt have many of.
+        for (size_t k = 0; k < pl->tiles.size();) {
+            const int32_t a = (int32_t)k, b2 = k + 1 < pl->tiles.size() && pl->tiles[k + 1].req == pl->tiles[k].req ? a + 1 : -1;
+            gap[a] = gap_at(a);
+            bool together = b2 >= 0 && (window == 0 || pl->tiles[b2].kv_full - window <= pl->tiles[a].kv_len);
+            if (together && window > 0) {
+                gap[b2] = gap_at(b2);
+                const int64_t apart = model_cycles(0, steps_of(a), 1) + model_cycles(0, steps_of(b2), 1);
+                gap[b2] = gap[a];
+                together = model_cycles(steps_of(a), steps_of(b2), 2) <= apart;
+            }
+            pairs.push_back({a, together ? b2 : -1});
+            k += together ? 2 : 1;
+        }
         // Split-KV: the key ranges of a batch that leaves SMs idle are cut into parts of at most `limit` steps
         // that run as separate items and are merged afterwards.
         //   items <= SMs / 2 : the smallest limit whose parts still fit one round (one item per SM), if the model gives
@@ -484,6 +508,8 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
             const int32_t req = pl->tiles[w.tile_a].req;
             w.seq_len = pl->seq_len[req];
             w.page_begin = pl->page_off[req];
+            w.gap = gap[w.tile_a];
+            w.sink_steps = w.gap > 0 ? sink_steps : 0;
         }
         // Launch latency is a visible part of a layer while the attention takes tens of microseconds: 240 items of up to 8
         // steps 53.0 -> 48.3 us a layer, 1 680 short items 121.1 -> 114.6.  Layers whose attention runs for hundreds, near

@@ -64,7 +64,9 @@ struct AttnWork {
     int32_t cost;      // (tile, step) count of the item: the host's sort key, not read by the kernel
     int32_t seq_len, page_begin;   // of the request: its length and first block-table entry (so that the loads of K and V
                                    // wait for this record and the page ids only, not for a chain through the tiles)
-    int32_t pad0, pad1;
+    // Of a plan with a window, steps are counted without those that no row of the item sees: step v stands for the keys from
+    // 128 v on while v < sink_steps, and from 128 (v + gap) on after that.  0 and 0 elsewhere.
+    int32_t sink_steps, gap;
 };
 
 // One (query tile, KV head) whose partial results have to be merged after a split-KV launch.
@@ -104,6 +106,7 @@ struct tessera_plan {
     tessera_model_cfg cfg{};
     std::vector<double> inv_freq;          // [D/2], always filled
     float sm_scale = 0.f;
+    int32_t window = 0, n_sink = 0;        // > 0: a query at p sees the keys k <= p with k < n_sink or k > p - window
     int32_t num_pool_pages = 0;
     int32_t num_source_pages = 0;          // > 0: cached units are read from a separate source pool
     int32_t batch = 0;
@@ -150,8 +153,9 @@ struct tessera_plan {
 namespace tessera {
 // Builds and validates all host tables.  Returns a status; on failure `err` holds the reason.
 // `num_sms`: multiprocessor count the work lists are sized for.  `may_cut`: key ranges may be cut (split-KV).
-int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc *desc,
-                        int32_t num_pool_pages, int num_sms, bool may_cut, tessera_plan *plan, std::string *err);
+// `window` 0: every query sees all keys up to its own.
+int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc *desc, int32_t num_pool_pages, int num_sms,
+                        bool may_cut, tessera_plan *plan, std::string *err, int32_t window = 0, int32_t n_sink = 0);
 
 // Thread blocks of an attention launch over the whole list (chunk < 0) or a chunk's: one per SM, `max_blocks` > 0 at most,
 // no more than items.  0 where the list cannot be walked by so few: a dealt list has holes that end a block's share only
