@@ -252,6 +252,26 @@ TESSERA_API int32_t tessera_kv_retain_fp8(const tessera_plan *plan, const void *
                                           void *v_dst8, float k_scale, float v_scale, uint32_t flags, void *stream);
 
 /*
+ * 4-bit storage tier: the same two directions with pools that hold 4-bit rows.  (No counterpart in the paper.)  A 4-bit
+ * pool is [num_pages][H_kv][page_size * (D/2 + 8)] bytes, 16-byte aligned: of a page and KV head first the codes of all its
+ * tokens, D/2 bytes each (byte i: element i in the low four bits, element i + D/2 in the high four), then four bf16 numbers for
+ * every token: scale and least value of the head's first half, then of its second.  A half x_0 .. x_{D/2-1} of a 16-bit row
+ * is kept as
+ *     least = min x,   scale = bf16_rne(fp32((max x - min x) / 15)),   c_i = min(15, nearest integer to (x_i - least) / scale)
+ * (ties to even; scale and codes 0 where the scale would be below 2^-126; a half that holds a NaN or an infinity, or whose range
+ * is above fp32's, gets scale = least = NaN), and a code stands for fp32(scale c + least), one rounding.
+ *   tessera_kv_retain_kv4        16-bit source pools -> 4-bit pools of num_pool_pages pages (the plan's destination).  With
+ *                                TESSERA_FUSE_ROPE keys are rotated by the plan's shifts and rounded to bf16 first.
+ *   tessera_kv_compose_from_kv4  4-bit source pools -> the request's 16-bit pages: bf16_rne of the value, keys of which are
+ *                                rotated in fp32 first with TESSERA_FUSE_ROPE.
+ * Both need a plan with desc.num_source_pages > 0; errors as tessera_kv_compose_from.  One kernel; nothing is allocated.
+ */
+TESSERA_API int32_t tessera_kv_retain_kv4(const tessera_plan *plan, const void *k_src, const void *v_src, void *k_dst4, void *v_dst4,
+                                          uint32_t flags, void *stream);
+TESSERA_API int32_t tessera_kv_compose_from_kv4(const tessera_plan *plan, const void *k_src4, const void *v_src4, void *k_pool,
+                                                void *v_pool, uint32_t flags, void *stream);
+
+/*
  * "Applying RoPE to the keys at their new positions" (Sec. 5.3; the fused placement kernel of
  * Sec. 6.1) as a call of its own: rotates, in place, the destination-page K rows of every cached
  * unit by (new position - cached position).  NOT idempotent: call exactly once after a compose
@@ -292,6 +312,79 @@ TESSERA_API int32_t tessera_rope_fresh(const tessera_plan *plan, void *q, void *
 TESSERA_API int32_t tessera_extend_write(const tessera_plan *plan, void *k_pool, void *v_pool, void *q,
                                          const void *k_new_raw, const void *v_new, void *k_cache, void *v_cache,
                                          void *stream);
+
+/*
+ * Fresh rows of a layer, as its projections leave them: n tokens (the plan's recompute rows, or one for every request of a
+ * decode step), heads side by side inside a row, rows q_row / k_row / v_row ELEMENTS apart - so that the three may be
+ * parts of one fused projection.  All pointers device, bf16, 16-byte aligned.
+ */
+typedef struct tessera_fresh_rows {
+    const void *q;              /* [n] rows of H_q x D; nullable: keys and values alone                  */
+    const void *k, *v;          /* [n] rows of H_kv x D, un-rotated keys; never written                  */
+    void *q_out;                /* [n][H_q][D]; may be q itself where q_row is H_q D                      */
+    int64_t q_row, k_row, v_row;/* multiples of 8, 0 = H_q D, H_kv D                                     */
+    const void *q_weight;       /* [D] weights of the per-head norm of q, respectively k; NULL: that one is  */
+    const void *k_weight;       /*     rotated as it is                                                  */
+    float eps;                  /* added to the mean square: finite, >= 0                                 */
+} tessera_fresh_rows;
+
+/*
+ * tessera_extend_write for layers that NORMALISE queries and keys per head before the rotation (the paper's models do not
+ * all): every head x of q and k becomes R(p) (w x / sqrt(mean x^2 + eps)), in fp32 with one round-to-nearest-even to bf16 at
+ * the end (angle, cosine and sine in fp64).  Values are bit copies.  q goes to q_out, k and v to the rows' destination slots;
+ * of captured units (desc.unit_retain_page_off) the normalised, un-rotated key, rounded to bf16, and the value go to the cache
+ * pages: what a later plan reuses with unit_cached_stride = 0.  With both weights NULL it differs from
+ * tessera_extend_write in where q goes.  One kernel; nothing is allocated.  Errors: TESSERA_INVALID_ARG.
+ */
+TESSERA_API int32_t tessera_extend_write_norm(const tessera_plan *plan, void *k_pool, void *v_pool, const tessera_fresh_rows *rows,
+                                              void *k_cache, void *v_cache, void *stream);
+
+/*
+ * DECODE: the step after a composed prompt's first token.  (The paper stops at that token; these calls have no counterpart in
+ * it.)  Everything that changes from step to step lives in device memory, so a step can be captured into a graph once and
+ * replayed while lengths and tables are updated in place.
+ */
+typedef struct tessera_decode_desc {
+    int32_t batch;
+    int32_t max_pages;           /* columns of block_table                                               */
+    const int32_t *block_table;  /* device [batch][max_pages]: request r's page of positions [c B, (c + 1) B)  */
+    const int32_t *seq_len;      /* device [batch]: tokens of the request, the newest included; its position is
+                                    seq_len - 1.  0 or less: no request in this place                     */
+    int32_t num_pool_pages;      /* pages of the pools; a table entry outside [0, num_pool_pages) is never followed */
+    int32_t window, n_sink;      /* window 0: the new token sees all positions; otherwise those above seq_len - 1 - window and
+                                    the first n_sink (tessera_plan_create_windowed)                        */
+} tessera_decode_desc;
+
+/*
+ * The new tokens' rows into their pages: k and q normalised (where weights are given) and rotated for position seq_len - 1 as in
+ * tessera_extend_write_norm, q to q_out, k and v to slot seq_len - 1 of the request.  Requests without a token, whose table
+ * has no such column or whose page is outside the pool are left out: nothing of theirs is written (q_out neither).
+ * No two requests may write one slot.  _kv4: the pools are 4-bit ones and keep the quantised form of the very rows that
+ * tessera_decode_write stores.  window and n_sink are ignored.  cfg: head_dim 64 or 128, rope_theta / inv_freq, rope_pairing.
+ */
+TESSERA_API int32_t tessera_decode_write(const tessera_model_cfg *cfg, const tessera_decode_desc *desc, void *k_pool, void *v_pool,
+                                         const tessera_fresh_rows *rows, void *stream);
+TESSERA_API int32_t tessera_decode_write_kv4(const tessera_model_cfg *cfg, const tessera_decode_desc *desc, void *k_pool4, void *v_pool4,
+                                             const tessera_fresh_rows *rows, void *stream);
+
+/*
+ * Attention of one query token a request over its pages:
+ *   out[r][h] = softmax(sm_scale * q[r][h] . K[visible][h/g]) . V[visible][h/g];  fp32 scores, sums and accumulators.
+ *   q, out: device [batch][H_q][D] bf16, q rotated; lse: device [batch][H_q] fp32, natural log, nullable.
+ * A request without a token (or none of whose visible keys has a page in the pool) gets out = 0 and lse = -inf.  Keys on
+ * pages outside the pool count as not visible; a length above max_pages * page_size counts as that.  Rows that are not
+ * visible are not read.  Results do not depend on the timing of the run.
+ *   workspace: device, tessera_decode_workspace_bytes (a function of head_dim and of the current device), 16-byte aligned,
+ *   contents irrelevant before and after; calls that may overlap on the GPU - two streams, two graphs - need one each.
+ * Two kernels on `stream`; nothing is allocated.  _kv4: the pools are 4-bit ones (see tessera_kv_retain_kv4).
+ * Errors: TESSERA_UNSUPPORTED_SHAPE, TESSERA_INVALID_ARG, TESSERA_CUDA_ERROR.
+ */
+TESSERA_API int32_t tessera_decode_workspace_bytes(const tessera_model_cfg *cfg, int64_t *bytes);
+TESSERA_API int32_t tessera_decode_attn(const tessera_model_cfg *cfg, const tessera_decode_desc *desc, const void *k_pool, const void *v_pool,
+                                        const void *q, void *out, float *lse, void *workspace, int64_t workspace_bytes, void *stream);
+TESSERA_API int32_t tessera_decode_attn_kv4(const tessera_model_cfg *cfg, const tessera_decode_desc *desc, const void *k_pool4,
+                                            const void *v_pool4, const void *q, void *out, float *lse, void *workspace,
+                                            int64_t workspace_bytes, void *stream);
 
 /*
  * Completing prefill (Sec. 5.3): the extend pass restricted to the recompute rows.

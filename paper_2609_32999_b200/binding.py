@@ -54,9 +54,23 @@ class PlanInfo(ctypes.Structure):
                 ("retained_tokens", ctypes.c_int64), ("attn_mma_pairs", ctypes.c_int64)]
 
 
+class FreshRows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_out", ctypes.c_void_p),
+                ("q_row", ctypes.c_int64), ("k_row", ctypes.c_int64), ("v_row", ctypes.c_int64),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float)]
+
+
+class DecodeDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("block_table", ctypes.c_void_p),
+                ("seq_len", ctypes.c_void_p), ("num_pool_pages", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("n_sink", ctypes.c_int32)]
+
+
 EXPORTS = ["tessera_plan_create", "tessera_plan_create_windowed", "tessera_plan_destroy", "tessera_plan_block_table", "tessera_plan_get_info",
            "tessera_plan_status", "tessera_kv_compose", "tessera_kv_compose_from", "tessera_kv_compose_from_fp8", "tessera_kv_retain_fp8", "tessera_rope_shift", "tessera_rope_fresh", "tessera_extend_write", "tessera_partial_prefill_attn", "tessera_kv_compose_k8", "tessera_partial_prefill_attn_k8",
            "tessera_composed_prefill_host", "tessera_composed_prefill_host_tier", "tessera_rope_shift_static", "tessera_selftest_bounded_wait", "tessera_last_error",
+           "tessera_kv_retain_kv4", "tessera_kv_compose_from_kv4", "tessera_extend_write_norm", "tessera_decode_write", "tessera_decode_write_kv4",
+           "tessera_decode_workspace_bytes", "tessera_decode_attn", "tessera_decode_attn_kv4",
            "tessera_launch_count"]
 
 _vp = ctypes.c_void_p
@@ -84,6 +98,13 @@ _lib.tessera_composed_prefill_host_tier.argtypes = [_vp, _vp, _vp, ctypes.c_int3
 _lib.tessera_rope_shift_static.argtypes = [ctypes.POINTER(ModelCfg), _vp, ctypes.c_int64, _vp, _vp, ctypes.c_int32,
                                            _I32P, ctypes.c_int32, _vp]
 _lib.tessera_selftest_bounded_wait.argtypes = [ctypes.c_int64, _I32P, ctypes.POINTER(ctypes.c_int64), _vp]
+_lib.tessera_kv_retain_kv4.argtypes = _lib.tessera_kv_compose_from_kv4.argtypes = [_vp, _vp, _vp, _vp, _vp, ctypes.c_uint32, _vp]
+_lib.tessera_extend_write_norm.argtypes = [_vp, _vp, _vp, ctypes.POINTER(FreshRows), _vp, _vp, _vp]
+_lib.tessera_decode_write.argtypes = _lib.tessera_decode_write_kv4.argtypes = [ctypes.POINTER(ModelCfg), ctypes.POINTER(DecodeDesc), _vp, _vp,
+                                                                               ctypes.POINTER(FreshRows), _vp]
+_lib.tessera_decode_workspace_bytes.argtypes = [ctypes.POINTER(ModelCfg), ctypes.POINTER(ctypes.c_int64)]
+_lib.tessera_decode_attn.argtypes = _lib.tessera_decode_attn_kv4.argtypes = [ctypes.POINTER(ModelCfg), ctypes.POINTER(DecodeDesc), _vp, _vp, _vp, _vp,
+                                                                             _vp, _vp, ctypes.c_int64, _vp]
 _lib.tessera_last_error.argtypes = [ctypes.c_char_p, ctypes.c_int32]
 _lib.tessera_launch_count.argtypes = []
 _lib.tessera_launch_count.restype = ctypes.c_int64
@@ -134,6 +155,38 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream or None
 
 
+def _model_cfg(sh, inv: Optional[np.ndarray]) -> ModelCfg:
+    return ModelCfg(sh.num_q_heads, sh.num_kv_heads, sh.head_dim, sh.page_size, float(sh.rope_theta),
+                    None if inv is None else inv.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
+                    int(sh.rope_pairing), float(sh.sm_scale))
+
+
+def _expect(what: str, t, device, dtypes, shape, rows: bool = False) -> None:
+    """Device, type and shape of a tensor; contiguous, or (rows) with heads side by side inside rows any distance apart."""
+    if t.device != device or str(t.dtype) not in dtypes or tuple(t.shape) != shape:
+        raise ValueError("%s: expected %s of %s on %s, got %s of %s on %s"
+                         % (what, shape, " / ".join(dtypes), device, tuple(t.shape), t.dtype, t.device))
+    if not (t.is_contiguous() or (rows and t.stride()[1:] == (shape[2], 1) and t.stride(0) >= shape[1] * shape[2])):
+        raise ValueError("%s: strides %s" % (what, tuple(t.stride())))
+
+
+_BF16, _I32, _F32, _BYTES = ("torch.bfloat16",), ("torch.int32",), ("torch.float32",), ("torch.uint8",)
+
+
+def _fresh_rows(sh, n: int, device, q, q_out, k, v, q_weight, k_weight, eps) -> FreshRows:
+    hq, h, d = sh.num_q_heads, sh.num_kv_heads, sh.head_dim
+    if q is not None:
+        _expect("q", q, device, _BF16, (n, hq, d), rows=True)
+        _expect("q_out", q_out, device, _BF16, (n, hq, d))
+    _expect("k_new", k, device, _BF16, (n, h, d), rows=True)
+    _expect("v_new", v, device, _BF16, (n, h, d), rows=True)
+    for what, t in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if t is not None:
+            _expect(what, t, device, _BF16, (d,))
+    row = [0 if n < 2 or t is None else t.stride(0) for t in (q, k, v)]
+    return FreshRows(_dev(q), _dev(k), _dev(v), None if q is None else _dev(q_out), *row, _dev(q_weight), _dev(k_weight), eps)
+
+
 class Plan:
     """tessera_plan_create / tessera_plan_destroy with host arrays taken from a Workload-like
     object (anything with the descriptor's field names and a `.shape` model description).  With `window` > 0
@@ -147,9 +200,8 @@ class Plan:
                        "free_pages")]
         a = self._keep
         self._inv = None if inv_freq is None else np.ascontiguousarray(inv_freq, dtype=np.float64)
-        cfg = ModelCfg(sh.num_q_heads, sh.num_kv_heads, sh.head_dim, sh.page_size, float(sh.rope_theta),
-                       None if self._inv is None else self._inv.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
-                       int(sh.rope_pairing), float(sh.sm_scale))
+        cfg = _model_cfg(sh, self._inv)
+        self.shape = sh
         opt = [None if getattr(w, f, None) is None else _arr(getattr(w, f))
                for f in ("unit_src_offset", "unit_target_stride", "unit_retain_page_off", "unit_retain_pages")]
         op = [None if x is None else _ptr(x) for x in opt]
@@ -210,6 +262,16 @@ class Plan:
         _check(_lib.tessera_kv_retain_fp8(self._h, _dev(k_src), _dev(v_src), _dev(k_dst8), _dev(v_dst8), k_scale, v_scale,
                                           FUSE_ROPE if fuse_rope else 0, _stream(stream)))
 
+    def kv_retain_kv4(self, k_src, v_src, k_dst4, v_dst4, fuse_rope: bool = True, stream=None) -> None:
+        """16-bit source pools -> 4-bit pools (pool4_shape); the plan's destination pages index the 4-bit pools."""
+        _check(_lib.tessera_kv_retain_kv4(self._h, _dev(k_src), _dev(v_src), _dev(k_dst4), _dev(v_dst4), FUSE_ROPE if fuse_rope else 0,
+                                          _stream(stream)))
+
+    def kv_compose_from_kv4(self, k_src4, v_src4, k_pool, v_pool, fuse_rope: bool = True, stream=None) -> None:
+        """Sources in 4-bit pools (pool4_shape), destinations in the 16-bit pools, keys rotated on the way."""
+        _check(_lib.tessera_kv_compose_from_kv4(self._h, _dev(k_src4), _dev(v_src4), _dev(k_pool), _dev(v_pool), FUSE_ROPE if fuse_rope else 0,
+                                                _stream(stream)))
+
     def rope_shift(self, k_pool, stream=None) -> None:
         _check(_lib.tessera_rope_shift(self._h, _dev(k_pool), _stream(stream)))
 
@@ -222,6 +284,13 @@ class Plan:
         and the raw rows of captured units to k_cache / v_cache (attention then runs with k_new = v_new = None)."""
         _check(_lib.tessera_extend_write(self._h, _dev(k_pool), _dev(v_pool), _dev(q), _dev(k_new_raw), _dev(v_new),
                                          _dev(k_cache), _dev(v_cache), _stream(stream)))
+
+    def extend_write_norm(self, k_pool, v_pool, q, q_out, k_new_raw, v_new, q_weight=None, k_weight=None, eps: float = 1e-6, k_cache=None,
+                          v_cache=None, stream=None) -> None:
+        """extend_write with per-head norms of q and k before the rotation, q written to q_out (q itself, or another tensor); q, k_new_raw and
+        v_new may be slices [n_q, heads, D] of a fused projection.  q None: keys and values alone."""
+        rows = _fresh_rows(self.shape, int(self.info.n_q), k_new_raw.device, q, q_out, k_new_raw, v_new, q_weight, k_weight, eps)
+        _check(_lib.tessera_extend_write_norm(self._h, _dev(k_pool), _dev(v_pool), ctypes.byref(rows), _dev(k_cache), _dev(v_cache), _stream(stream)))
 
     def partial_prefill_attn(self, k_pool, v_pool, q, k_new, v_new, out, lse=None, stream=None) -> None:
         _check(_lib.tessera_partial_prefill_attn(self._h, _dev(k_pool), _dev(v_pool), _dev(q), _dev(k_new),
@@ -265,6 +334,83 @@ class Plan:
             self.destroy()
         except Exception:
             pass
+
+
+def pool4_shape(shape, num_pages: int):
+    """Shape of a 4-bit pool (uint8) of num_pages pages."""
+    return (int(num_pages), shape.num_kv_heads, shape.page_size * (shape.head_dim // 2 + 8))
+
+
+class Decode:
+    """The step after the first token (tessera_decode_*): one new token a request.
+
+    block_table [batch, max_pages] and seq_lens [batch] are int32 device tensors that the caller goes on updating in place;
+    they are read by every call when it runs on the GPU, so a step may be captured into a graph.  seq_lens counts the new
+    token, whose position is seq_lens - 1; 0 leaves a place out.  `workspace` (uint8, workspace_bytes(shape); made here by
+    default) must not be shared by calls that can overlap on the GPU: use a Decode for each stream or concurrent graph.
+    All tensors live on the device of block_table, which is the current one during the calls."""
+
+    def __init__(self, shape, block_table, seq_lens, num_pool_pages: int, window: int = 0, n_sink: int = 0, inv_freq=None, workspace=None):
+        import torch
+        self.shape, self.batch, self.device = shape, int(seq_lens.shape[0]), block_table.device
+        if block_table.device.type != "cuda" or block_table.dim() != 2:
+            raise ValueError("block_table: a [batch, max_pages] tensor on a CUDA device")
+        _expect("block_table", block_table, self.device, _I32, (self.batch, int(block_table.shape[1])))
+        _expect("seq_lens", seq_lens, self.device, _I32, (self.batch,))
+        self._index, self._current = self.device.index, torch._C._cuda_getDevice
+        # (the frequencies here, once: 64 powers in every call's host time otherwise)
+        d = shape.head_dim
+        self._inv = np.ascontiguousarray([float(shape.rope_theta) ** (-2.0 * m / d) for m in range(d // 2)] if inv_freq is None else inv_freq, dtype=np.float64)
+        self._cfg = _model_cfg(shape, self._inv)
+        self.block_table, self.seq_lens, self.num_pool_pages = block_table, seq_lens, int(num_pool_pages)
+        self._desc = DecodeDesc(self.batch, int(block_table.shape[1]), _dev(block_table), _dev(seq_lens), self.num_pool_pages, int(window), int(n_sink))
+        need = ctypes.c_int64(0)
+        with torch.cuda.device(self.device):
+            _check(_lib.tessera_decode_workspace_bytes(ctypes.byref(self._cfg), ctypes.byref(need)))
+        self.workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device) if workspace is None else workspace
+        _expect("workspace", self.workspace, self.device, _BYTES, (int(self.workspace.numel()),))
+        self._pool = (self.num_pool_pages, shape.page_size, shape.num_kv_heads, d)
+        self._pool4 = pool4_shape(shape, self.num_pool_pages)
+        self._q = (self.batch, shape.num_q_heads, d)
+
+    def _pools(self, k_pool, v_pool, dtypes, shape) -> None:
+        if self._current() != self._index:
+            raise ValueError("the current device is not %s" % self.device)
+        _expect("k_pool", k_pool, self.device, dtypes, shape)
+        _expect("v_pool", v_pool, self.device, dtypes, shape)
+
+    def _write(self, call, k_pool, v_pool, q, q_out, k_new, v_new, q_weight, k_weight, eps, stream) -> None:
+        rows = _fresh_rows(self.shape, self.batch, self.device, q, q_out, k_new, v_new, q_weight, k_weight, eps)
+        _check(call(ctypes.byref(self._cfg), ctypes.byref(self._desc), _dev(k_pool), _dev(v_pool), ctypes.byref(rows), _stream(stream)))
+
+    def write(self, k_pool, v_pool, q, q_out, k_new, v_new, q_weight=None, k_weight=None, eps: float = 1e-6, stream=None) -> None:
+        """The new tokens' un-rotated rows: q (normalised with q_weight, rotated) to q_out, k (likewise) and v to their slots.  q, k_new and v_new
+        may be slices [batch, heads, D] of a fused projection; q None: keys and values alone."""
+        self._pools(k_pool, v_pool, _BF16, self._pool)
+        self._write(_lib.tessera_decode_write, k_pool, v_pool, q, q_out, k_new, v_new, q_weight, k_weight, eps, stream)
+
+    def write_kv4(self, k_pool4, v_pool4, q, q_out, k_new, v_new, q_weight=None, k_weight=None, eps: float = 1e-6, stream=None) -> None:
+        """write() into 4-bit pools (pool4_shape)."""
+        self._pools(k_pool4, v_pool4, _BYTES, self._pool4)
+        self._write(_lib.tessera_decode_write_kv4, k_pool4, v_pool4, q, q_out, k_new, v_new, q_weight, k_weight, eps, stream)
+
+    def _attn(self, call, k_pool, v_pool, q, out, lse, stream) -> None:
+        _expect("q", q, self.device, _BF16, self._q)
+        _expect("out", out, self.device, _BF16, self._q)
+        if lse is not None:
+            _expect("lse", lse, self.device, _F32, self._q[:2])
+        _check(call(ctypes.byref(self._cfg), ctypes.byref(self._desc), _dev(k_pool), _dev(v_pool), _dev(q), _dev(out), _dev(lse),
+                    _dev(self.workspace), self.workspace.numel(), _stream(stream)))
+
+    def attn(self, k_pool, v_pool, q, out, lse=None, stream=None) -> None:
+        """Attention of the rotated q [batch, H_q, D] over the requests' 16-bit pages."""
+        self._pools(k_pool, v_pool, _BF16, self._pool)
+        self._attn(_lib.tessera_decode_attn, k_pool, v_pool, q, out, lse, stream)
+
+    def attn_kv4(self, k_pool4, v_pool4, q, out, lse=None, stream=None) -> None:
+        """Attention of the rotated q [batch, H_q, D] over the requests' 4-bit pages (pool4_shape)."""
+        self._pools(k_pool4, v_pool4, _BYTES, self._pool4)
+        self._attn(_lib.tessera_decode_attn_kv4, k_pool4, v_pool4, q, out, lse, stream)
 
 
 def selftest_bounded_wait(max_cycles: int, stream=None):

@@ -17,6 +17,7 @@
 
 #include "device_mem.cuh"
 #include "launch.h"
+#include "pair_chunk.cuh"
 #include "plan.h"
 
 namespace tessera {
@@ -25,24 +26,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ void unpack_bf16x8(const uint4 &v, float (&f)[8]) {
-    const uint32_t *w = reinterpret_cast<const uint32_t *>(&v);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ uint4 pack_bf16x8(const float (&f)[8]) {
-    uint4 v;
-    uint32_t *w = reinterpret_cast<uint32_t *>(&v);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-        w[i] = *reinterpret_cast<uint32_t *>(&p);
-    }
-    return v;
-}
 // 8 codes -> 8 floats (exact) times mul (one fp32 rounding).
 __device__ __forceinline__ void unpack_e4m3x8(const uint2 &v, float mul, float (&f)[8]) {
     const uint32_t w[2] = {v.x, v.y};
@@ -65,33 +48,6 @@ __device__ __forceinline__ uint2 pack_e4m3x8(const float (&f)[8], float mul) {
         w[i >> 1] |= two << (16 * (i & 1));
     }
     return make_uint2(w[0], w[1]);
-}
-
-// x' = x cos - y sin, y' = y cos + x sin in fp32, the arithmetic of the 16-bit gather; a table entry
-// that is exactly (1, 0) leaves the pair untouched (signed zeros and infinities survive a zero shift).
-__device__ __forceinline__ void rotate_pair(float &x, float &y, const float2 c) {
-    const bool identity = c.x == 1.f && c.y == 0.f;
-    const float a = fmaf(-y, c.y, x * c.x), b = fmaf(x, c.y, y * c.x);
-    x = identity ? x : a;
-    y = identity ? y : b;
-}
-template <bool INTERLEAVED>
-__device__ __forceinline__ void rotate_f(float (&lo)[8], float (&hi)[8], const float2 *cs) {
-    if (INTERLEAVED) {
-        // lo holds pairs (0,1) (2,3) .. with cs[0..3]; hi the chunk D/2 elements later with cs[4..7]
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            rotate_pair(lo[2 * i], lo[2 * i + 1], cs[i]);
-            rotate_pair(hi[2 * i], hi[2 * i + 1], cs[4 + i]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) rotate_pair(lo[i], hi[i], cs[i]);
-    }
-}
-template <int D, bool INTERLEAVED>
-__device__ __forceinline__ int cs_index(int c, int i) {
-    return INTERLEAVED ? (i < 4 ? 4 * c + i : 4 * c + D / 4 + (i - 4)) : c * 8 + i;
 }
 
 // A load of one 16-element task's half row: D / 16 neighbouring threads read the half of a head, T each.  Where that is
@@ -176,7 +132,7 @@ kv_fp8_kernel(const void *__restrict__ k_src, const void *__restrict__ v_src, vo
                 const float2 *row = s_rope + (size_t)sr * (D / 2);
                 float2 cr[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) cr[i] = row[cs_index<D, INTERLEAVED>(c, i)];
+                for (int i = 0; i < 8; ++i) cr[i] = row[cs_entry<D, INTERLEAVED>(c, i)];
                 rotate_f<INTERLEAVED>(klo, khi, cr);
             }
             if constexpr (TO_8BIT) {
@@ -240,7 +196,7 @@ expand_runs_kernel(const uint2 *__restrict__ k_src, const uint2 *__restrict__ v_
                     const float2 *row = rope + (size_t)(it.row0 + tok * it.row_step) * (D / 2);
                     float2 cr[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) cr[i] = row[cs_index<D, INTERLEAVED>(c, i)];
+                    for (int i = 0; i < 8; ++i) cr[i] = row[cs_entry<D, INTERLEAVED>(c, i)];
                     float lo[8], hi[8];
                     unpack_e4m3x8(rk[u][0], k_mul, lo);
                     unpack_e4m3x8(rk[u][1], k_mul, hi);

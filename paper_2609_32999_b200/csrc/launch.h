@@ -14,11 +14,11 @@ void count_launch();   // bumps the process-wide kernel-launch counter
 // (the kernel itself waits, see grid_wait()); behind anything but a kernel that is an ordinary launch too.
 // `cluster`: thread blocks per cluster (2: blocks 2 i and 2 i + 1 run on the two SMs of one TPC).
 template <class... P, class... A>
-cudaError_t launch_clusters(void (*kernel)(P...), unsigned grid, unsigned block, unsigned cluster, size_t smem, cudaStream_t st,
+cudaError_t launch_clusters(void (*kernel)(P...), dim3 grid, unsigned block, unsigned cluster, size_t smem, cudaStream_t st,
                             bool chained, A... args) {
     cudaLaunchAttribute attr[2]{};
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
@@ -40,6 +40,10 @@ cudaError_t launch_clusters(void (*kernel)(P...), unsigned grid, unsigned block,
 }
 template <class... P, class... A>
 cudaError_t launch_kernel(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, bool chained, A... args) {
+    return launch_clusters(kernel, dim3(grid), block, 1, smem, st, chained, args...);
+}
+template <class... P, class... A>
+cudaError_t launch_grid(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, bool chained, A... args) {
     return launch_clusters(kernel, grid, block, 1, smem, st, chained, args...);
 }
 
