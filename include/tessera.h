@@ -374,9 +374,10 @@ TESSERA_API int32_t tessera_decode_write_kv4(const tessera_model_cfg *cfg, const
  * A request without a token (or none of whose visible keys has a page in the pool) gets out = 0 and lse = -inf.  Keys on
  * pages outside the pool count as not visible; a length above max_pages * page_size counts as that.  Rows that are not
  * visible are not read.  Results do not depend on the timing of the run.
- *   workspace: device, tessera_decode_workspace_bytes (a function of head_dim and of the current device), 16-byte aligned,
- *   contents irrelevant before and after; calls that may overlap on the GPU - two streams, two graphs - need one each.
- * Two kernels on `stream`; nothing is allocated.  _kv4: the pools are 4-bit ones (see tessera_kv_retain_kv4).
+ *   workspace: device, tessera_decode_workspace_bytes (a function of head_dim and of the current device), 16-byte aligned.  It must
+ *   be all zeros before its first use; every call leaves it ready for the next (captured ones too), and in between it must not be
+ *   written.  Calls that may overlap on the GPU - two streams, two graphs - need one each.
+ * One kernel on `stream`; nothing is allocated.  _kv4: the pools are 4-bit ones (see tessera_kv_retain_kv4).
  * Errors: TESSERA_UNSUPPORTED_SHAPE, TESSERA_INVALID_ARG, TESSERA_CUDA_ERROR.
  */
 TESSERA_API int32_t tessera_decode_workspace_bytes(const tessera_model_cfg *cfg, int64_t *bytes);

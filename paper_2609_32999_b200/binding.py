@@ -346,8 +346,8 @@ class Decode:
 
     block_table [batch, max_pages] and seq_lens [batch] are int32 device tensors that the caller goes on updating in place;
     they are read by every call when it runs on the GPU, so a step may be captured into a graph.  seq_lens counts the new
-    token, whose position is seq_lens - 1; 0 leaves a place out.  `workspace` (uint8, workspace_bytes(shape); made here by
-    default) must not be shared by calls that can overlap on the GPU: use a Decode for each stream or concurrent graph.
+    token, whose position is seq_lens - 1; 0 leaves a place out.  `workspace` (uint8, all zeros before its first use; made
+    here by default) must not be shared by calls that can overlap on the GPU: use a Decode for each stream or concurrent graph.
     All tensors live on the device of block_table, which is the current one during the calls."""
 
     def __init__(self, shape, block_table, seq_lens, num_pool_pages: int, window: int = 0, n_sink: int = 0, inv_freq=None, workspace=None):
@@ -367,7 +367,7 @@ class Decode:
         need = ctypes.c_int64(0)
         with torch.cuda.device(self.device):
             _check(_lib.tessera_decode_workspace_bytes(ctypes.byref(self._cfg), ctypes.byref(need)))
-        self.workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device) if workspace is None else workspace
+        self.workspace = torch.zeros(need.value, dtype=torch.uint8, device=self.device) if workspace is None else workspace
         _expect("workspace", self.workspace, self.device, _BYTES, (int(self.workspace.numel()),))
         self._pool = (self.num_pool_pages, shape.page_size, shape.num_kv_heads, d)
         self._pool4 = pool4_shape(shape, self.num_pool_pages)

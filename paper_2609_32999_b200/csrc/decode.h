@@ -6,7 +6,7 @@
 
 namespace tessera {
 
-constexpr int kDecodeUnit = 64;      // keys of the unit in which a decode step's work is handed out
+constexpr int kDecodeUnit = 16;      // keys of the tile in which a decode step's work is handed out
 
 // Shapes, ranges and pointers of a decode call; on failure `err` holds the reason.
 int32_t check_decode(const tessera_model_cfg *cfg, const tessera_decode_desc *desc, std::string *err);
