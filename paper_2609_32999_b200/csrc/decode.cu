@@ -21,6 +21,7 @@
 #include <cmath>
 #include <cstring>
 #include <string>
+#include <type_traits>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -40,6 +41,8 @@ int32_t api_set_error(int32_t code, const std::string &msg);
 namespace {
 
 constexpr int kTile = kDecodeUnit;
+constexpr float kValueUnit = 18446744073709551616.f;                 // 2^64: products with subnormal codes come out near 2^-69
+constexpr float kValueTop = 5192296858534827628530496329220096.f;    // 2^112: p (at most 2^8) times this is a bf16 number
 constexpr int kMaxGroup = 16;
 
 struct Args {
@@ -79,8 +82,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const void *src, bool there) {
-    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+// N bytes to shared memory; zeros in place of what is not there.
+template <int N, bool ALL> __device__ __forceinline__ void cp_async(uint32_t dst, const void *src, bool there) {
+    if constexpr (N == 16 && ALL) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+    else if constexpr (ALL) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(there ? 8 : 0) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -106,15 +112,6 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Four-bit codes at bits 0-3 and 16-19 -> two bf16 numbers c - 8, exact: a code in the last bits of 128's mantissa is 128 + c.
-__device__ __forceinline__ uint32_t codes_centred(uint32_t w) {
-    uint32_t x;
-    asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xea;" : "=r"(x) : "r"(w));     // (w & mask) | bits
-    const uint32_t mid = 0x43084308u;                                              // 136
-    const __nv_bfloat162 y = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&mid));
-    return *reinterpret_cast<const uint32_t *>(&y);
-}
-
 // A request's visible keys: k < len with k < sinks or k >= first; its tiles: the first `front` of the request's, then those from
 // `front + skip` on, n in all.
 struct Visible { int len, first, sinks, n, front, skip; };
@@ -129,12 +126,18 @@ __device__ __forceinline__ Visible visible(int len, const Args &a) {
 // Where in the batch a tile lies: request, tiles of the requests before it.
 struct Start { int request, before; };
 
-// A stage's contents: rows that are there (bit i: row i), whether the tile is its pair's first and last, and the pair.
-struct Meta { uint32_t rows; int pair, begin, tiles; };          // begin: tiles of the batch before the pair's
+// Of a stage: rows that are there (bit i: row i), and whether the tile is its pair's first and last.
 constexpr uint32_t kFirst = 1u << 30, kLast = 1u << 31;
 
-// A warp's part of a pair (tiles < 0: none) that begins, respectively ends, elsewhere.
-struct Part { int pair, begin, tiles; };
+// A pair: its number, tiles of the batch before its first, its tiles (of a warp's part: < 0, there is none).
+struct Pair { int pair, begin, tiles; };
+
+// Worker i of the batch has the tiles from all i / workers (rounded down) on; both factors of the product below 2^15.
+__device__ __forceinline__ int first_tile(int i, int workers, int all) {
+    if (workers == 0) return 0;
+    const uint32_t whole = (uint32_t)all / workers, rest = (uint32_t)all % workers;
+    return (int)(whole * i + rest * i / workers);
+}
 
 // The tiles of the block's warps, [s_first[w], s_first[w + 1]), and where each begins.  Returns the number of tiles of the batch.
 // Sums run over the batch in chunks of a block's threads.  (Where there are fewer tiles than warps the first warps have one each.)
@@ -171,7 +174,7 @@ __device__ __forceinline__ int shares(const Args &a, int *s_first, Start *s_star
     const int workers = min((int)gridDim.x * W, all);
     if (tid <= W) {
         const int i = min((int)blockIdx.x * W + tid, workers);
-        s_first[tid] = workers > 0 ? (int)((int64_t)all * i / workers) : 0;
+        s_first[tid] = first_tile(i, workers, all);
     }
     __syncthreads();
     for (int r0 = 0, before = 0; r0 < a.batch && before <= s_first[W - 1]; r0 += NT, before += chunk) {
@@ -192,15 +195,17 @@ __device__ __forceinline__ int shares(const Args &a, int *s_first, Start *s_star
     return all;
 }
 
-template <int D, bool F4, int NQ>
+template <int D, bool F4, int NQ, bool P8>
 __global__ void __launch_bounds__(Geo<D, F4, NQ>::kThreads, 1)
 decode_attn_kernel(const __grid_constant__ Args a) {
     using G = Geo<D, F4, NQ>;
     constexpr int NW = G::kWarps, NT = G::kThreads, CPR = G::kRow / 16, Q8 = 8 * NQ, KS = D / 16, RP = D + 4;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ Meta s_meta[NW][G::kStages];
+    __shared__ uint32_t s_flags[NW][G::kStages];
+    __shared__ Pair s_pair[NW][G::kStages];           // of a stage that is its pair's first, or the warp's
     __shared__ float2 s_ml[NW][2][Q8];
-    __shared__ Part s_part[NW][2];                    // [0]: of a pair that began before the warp's stretch, [1]: of one that goes on behind it
+    __shared__ float2 s_all[Q8];                      // reference and sum of a chain
+    __shared__ Pair s_part[NW][2];                    // [0]: of a pair that began before the warp's stretch, [1]: of one that goes on behind it
     __shared__ Start s_start[NW];
     __shared__ int s_first[NW + 1], s_sum[NW], s_last;
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, quad = lane / 4, t = lane % 4;
@@ -214,64 +219,67 @@ decode_attn_kernel(const __grid_constant__ Args a) {
     float *part0 = reinterpret_cast<float *>(smem + G::kRing) + warp * G::kPart;
 
     if (my_tiles > 0) {
-        // ---- the warp's fetching end: where the next tile to be sent for lies, and its page ids
-        int r = s_start[warp].request, base = s_start[warp].before, sent = 0, h, j, page0, page1;
+        // ---- the warp's fetching end: where the next tile to be sent for lies, and the page ids of 32 tiles from jb on, one a lane
+        // (P8: pages of 8 tokens, two a tile)
+        int r = s_start[warp].request, base = s_start[warp].before, sent = 0, h, j, jb, page_a, page_b = 0;
         Visible vis = visible(a.seq_len[r], a);
         h = (s_first[warp] - base) / vis.n;
-        j = (s_first[warp] - base) - h * vis.n;
+        j = jb = (s_first[warp] - base) - h * vis.n;
+        auto tile_at = [&](int i) { return i < vis.front ? i : i + vis.skip; };
         auto load_pages = [&]() {
             const int32_t *table = a.table + (size_t)r * a.max_pages;
-            const int key0 = (j < vis.front ? j : j + vis.skip) * kTile;
-            page0 = table[key0 >> page_shift];
-            page1 = key0 + 8 < vis.len ? table[(key0 + 8) >> page_shift] : -1;
+            const int i = jb + lane, key0 = tile_at(i) * kTile;
+            page_a = i < vis.n ? table[key0 >> page_shift] : -1;
+            if (P8) page_b = i < vis.n && key0 + 8 < vis.len ? table[(key0 >> page_shift) + 1] : -1;
         };
         load_pages();
+        // A lane's own places: of its 16 bytes of the rows (and its 8 of their numbers) in page 0 of head h.
+        constexpr int RPT = 32 / CPR;              // rows a turn of 32 lanes
+        const uint32_t head_bytes = F4 ? (uint32_t)a.page_size * (D / 2 + 8) : (uint32_t)G::kRow;
+        const uint32_t row_bytes = F4 ? (uint32_t)G::kRow : a.H_kv * head_bytes, page_bytes = F4 ? a.H_kv * head_bytes : row_bytes << page_shift;
+        const uint32_t place = (lane / CPR) * row_bytes + lane % CPR * 16;
+        const uint32_t place4 = (uint32_t)a.page_size * (D / 2) + (lane & 15) * 8;
         auto fetch = [&](int at) {
             if (sent < my_tiles) {
-                const int key0 = (j < vis.front ? j : j + vis.skip) * kTile, key = key0 + (lane & 15), page = lane & 8 ? page1 : page0;
-                const bool there_l = key < vis.len && (key < vis.sinks || key >= vis.first) && page >= 0 && page < a.num_pool_pages;
-                const uint32_t rows = __ballot_sync(0xffffffffu, there_l) & 0xffffu;
-                if (lane == 0)
-                    s_meta[warp][at] = {rows | (j == 0 ? kFirst : 0u) | (j == vis.n - 1 ? kLast : 0u), r * a.H_kv + h, base + h * vis.n, vis.n};
-                // (rows 0-7 and 8-15 of a tile lie side by side in one page each; of a page that is not there nothing is read)
-                const size_t p0 = (rows & 0x00ffu) ? page0 : 0, p1 = (rows & 0xff00u) ? page1 : 0;
-                const int off0 = key0 & (a.page_size - 1), off1 = (key0 + 8) & (a.page_size - 1);
+                const int key0 = tile_at(j) * kTile, off = key0 & (a.page_size - 1), pa = __shfl_sync(0xffffffffu, page_a, j - jb);
+                const int pb = P8 ? __shfl_sync(0xffffffffu, page_b, j - jb) : pa;
+                auto in_pool = [&](int page) { return (uint32_t)page < (uint32_t)a.num_pool_pages; };
+                uint32_t rows = 0xffffu;
+                if (!(in_pool(pa) && (!P8 || in_pool(pb)) && key0 + kTile <= vis.len && (key0 >= vis.first || key0 + kTile <= vis.sinks))) {
+                    const int key = key0 + (lane & 15);
+                    rows = __ballot_sync(0xffffffffu, key < vis.len && (key < vis.sinks || key >= vis.first) && in_pool(lane & 8 ? pb : pa)) & 0xffffu;
+                }
+                if (lane == 0) s_flags[warp][at] = rows | (j == 0 ? kFirst : 0u) | (j == vis.n - 1 ? kLast : 0u);
+                if ((j == 0 || sent == 0) && lane == 0) s_pair[warp][at] = {r * a.H_kv + h, base + h * vis.n, vis.n};
                 const uint32_t kb = ring + at * G::kStageBytes, vb = kb + kTile * G::kRow;
-                if constexpr (F4) {
-                    const size_t o0 = codes4_at<D>(p0, off0, h, a.page_size, a.H_kv), o1 = codes4_at<D>(p1, off1, h, a.page_size, a.H_kv);
-#pragma unroll
-                    for (int i = 0; i < kTile * CPR / 32; ++i) {
-                        // D 128: 8 rows a turn; 64: all 16 rows at once
-                        const int idx = i * 32 + lane, row = idx / CPR, c = idx % CPR;
-                        const bool there = (rows >> row) & 1;
-                        const size_t o = (row < 8 ? o0 : o1) + (row & 7) * G::kRow + c * 16;
-                        cp_async<16>(kb + row * G::kRow + c * 16, a.k + o, there);
-                        // (the halves of rows 4-7 of 8 change places: the four rows and eight columns that a warp's lanes ask for at once
-                        // then lie in different banks)
-                        const int cv = D == 128 ? c ^ (((row >> 2) & 1) << 1) : c;
-                        cp_async<16>(vb + row * G::kRow + cv * 16, a.v + o, there);
-                    }
-                    const int row = lane & 15;
-                    const size_t po = row < 8 ? params4_at<D>(p0, off0 + row, h, a.page_size, a.H_kv) : params4_at<D>(p1, off1 + row - 8, h, a.page_size, a.H_kv);
-                    cp_async<8>(vb + kTile * G::kRow + lane * 8, (lane < 16 ? a.k : a.v) + po, (rows >> row) & 1);
-                } else {
-                    constexpr int RPT = 32 / CPR;              // rows a turn
-                    const int row0 = lane / CPR, c = lane % CPR;
-                    const size_t o0 = ((((size_t)p0 << page_shift) + off0 + row0) * a.H_kv + h) * G::kRow + c * 16;
-                    const size_t o1 = ((((size_t)p1 << page_shift) + off1 + row0) * a.H_kv + h) * G::kRow + c * 16;
-                    const int step = RPT * a.H_kv * G::kRow;
+                auto copy = [&](auto all_there) {
+                    constexpr bool ALL = decltype(all_there)::value;
+                    // (of a page that is not there nothing is read)
+                    const uint64_t p0 = (uint64_t)(ALL || in_pool(pa) ? (uint32_t)pa : 0u) * page_bytes + h * head_bytes + off * (uint64_t)row_bytes + place;
+                    const uint64_t p1 = P8 ? (uint64_t)(ALL || in_pool(pb) ? (uint32_t)pb : 0u) * page_bytes + h * head_bytes + place : p0 + 8 * (uint64_t)row_bytes;
 #pragma unroll
                     for (int i = 0; i < kTile / RPT; ++i) {
-                        const int row = i * RPT + row0, cs = c ^ (row & 7);
-                        const bool there = (rows >> row) & 1;
-                        const size_t o = (i * RPT < 8 ? o0 + (size_t)(i * step) : o1 + (size_t)((i - 8 / RPT) * step));
-                        cp_async<16>(kb + row * G::kRow + cs * 16, a.k + o, there);
-                        cp_async<16>(vb + row * G::kRow + cs * 16, a.v + o, there);
+                        const int row = i * RPT + lane / CPR, c = lane % CPR;
+                        // a lane's rows of this turn: all in one half of the tile, but where a turn is the whole tile
+                        const uint64_t o = RPT == 16 ? (lane < 16 || !P8 ? p0 : p1 - 8 * (uint64_t)row_bytes) : i * RPT < 8 ? p0 + (uint64_t)(i * RPT) * row_bytes : p1 + (uint64_t)(i * RPT - 8) * row_bytes;
+                        // 16-bit: chunks turned by the row, as ldmatrix wants them; 4-bit values: the halves of rows 4-7 of 8 change places, so
+                        // that the four rows and eight columns that a warp's lanes ask for at once lie in different banks
+                        const int ck = F4 ? c : c ^ (row & 7), cv = F4 ? (D == 128 ? c ^ (((row >> 2) & 1) << 1) : c) : ck;
+                        cp_async<16, ALL>(kb + row * G::kRow + ck * 16, a.k + o, (rows >> row) & 1);
+                        cp_async<16, ALL>(vb + row * G::kRow + cv * 16, a.v + o, (rows >> row) & 1);
                     }
-                }
+                    if constexpr (F4) {
+                        const bool second = P8 && (lane & 8);
+                        const uint64_t o = (uint64_t)(ALL || in_pool(second ? pb : pa) ? (uint32_t)(second ? pb : pa) : 0u) * page_bytes + h * head_bytes + (second ? -64 : off * 8) + place4;
+                        cp_async<8, ALL>(vb + kTile * G::kRow + lane * 8, (lane < 16 ? a.k : a.v) + o, (rows >> (lane & 15)) & 1);
+                    }
+                };
+                if (rows == 0xffffu) copy(std::true_type{});
+                else copy(std::false_type{});
                 if (++sent < my_tiles) {
                     if (++j == vis.n) {
-                        j = 0;
+                        const bool same = jb == 0 && h + 1 < a.H_kv;          // the next head's pages are the ones at hand
+                        j = jb = 0;
                         if (++h == a.H_kv) {
                             h = 0;
                             do {
@@ -279,8 +287,11 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                                 vis = visible(a.seq_len[++r], a);
                             } while (vis.n == 0);
                         }
+                        if (!same) load_pages();
+                    } else if (j - jb == 32) {
+                        jb = j;
+                        load_pages();
                     }
-                    load_pages();
                 }
             }
             cp_commit();
@@ -291,7 +302,8 @@ decode_attn_kernel(const __grid_constant__ Args a) {
         float q_sum[NQ][2][2];           // 4-bit: sums of q over each half, of columns 2 t and 2 t + 1, in units of `unit`
         float unit[NQ][2];               // score times scale log2(e) per score sum: scale_log2, 4-bit: by column, for q's and the codes' scaling
         float m[NQ][2], l[NQ][2], off[NQ][2][2];         // off (4-bit): sums of p times a half's middle value
-        float acc[NQ][D / 16][4];
+        float acc[NQ][D / 16][4];        // 4-bit: times v_unit 2^-133, second half 2^-129
+        float v_unit = kValueUnit;
 
         auto begin_pair = [&](int pair) {
             const int qr = pair / a.H_kv, qh = pair - qr * a.H_kv;
@@ -358,6 +370,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                         for (int i = 0; i < 2; ++i) qf[n][s][i] = there ? *reinterpret_cast<const uint32_t *>(q + 16 * s + 8 * i + 2 * t) : 0u;
                     unit[n][0] = unit[n][1] = a.scale_log2;
                 }
+                v_unit = kValueUnit;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) m[n][e] = -INFINITY, l[n][e] = off[n][0][e] = off[n][1][e] = 0.f;
 #pragma unroll
@@ -380,8 +393,12 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                     l[n][e] = column_sum(l[n][e]);
                     if constexpr (F4) {
                         const float o[2] = {column_sum(off[n][0][e]), column_sum(off[n][1][e])};
+                        const float back = kValueUnit / v_unit;
 #pragma unroll
-                        for (int d = 0; d < D / 16; ++d) acc[n][d][e] += o[d / (D / 32)], acc[n][d][e + 2] += o[d / (D / 32)];
+                        for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)          // 2^133 / v_unit, 2^129 / v_unit
+                                acc[n][d][e + 2 * i] = fmaf(acc[n][d][e + 2 * i] * (d < D / 32 ? 5.9029581035870565e20f : 3.6893488147419103e19f), back, o[d / (D / 32)]);
                     }
                 }
         };
@@ -427,7 +444,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                 }
             }
         };
-        auto keep_part = [&](int which, float *to, const Meta &mt) {
+        auto keep_part = [&](int which, float *to, const Pair &now) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -440,21 +457,24 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                         to[col * RP + element(d, 1)] = acc[n][d][e + 2];
                     }
                 }
-            if (lane == 0) s_part[warp][which] = {mt.pair, mt.begin, mt.tiles};
+            if (lane == 0) s_part[warp][which] = now;
         };
 
+        begin_pair(r * a.H_kv + h);           // (q comes in beside the page ids)
 #pragma unroll
         for (int s = 0; s < G::kStages - 1; ++s) fetch(s);
         bool begun_here = false;
+        Pair now{};
         int at = 0;
         for (int s = 0; s < my_tiles; ++s) {
             cp_wait<G::kStages - 2>();
             __syncwarp();
             fetch(at == 0 ? G::kStages - 1 : at - 1);      // into the stage consumed in the last turn
-            const Meta mt = s_meta[warp][at];
-            if (s == 0 || (mt.rows & kFirst)) {
-                begin_pair(mt.pair);
-                begun_here = (mt.rows & kFirst) != 0;
+            const uint32_t flags = s_flags[warp][at];
+            if (s == 0 || (flags & kFirst)) {
+                now = s_pair[warp][at];
+                begun_here = (flags & kFirst) != 0;
+                if (s > 0) begin_pair(now.pair);
             }
             const uint32_t kb = ring + at * G::kStageBytes, vb = kb + kTile * G::kRow;
             const uint8_t *kp8 = smem + (kb - smem0), *vp8 = smem + (vb - smem0);
@@ -516,8 +536,8 @@ decode_attn_kernel(const __grid_constant__ Args a) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) sc[n][e] += odd[n][e];
             }
-            if ((mt.rows & 0xffffu) != 0xffffu) {
-                const bool here[2] = {((mt.rows >> row0) & 1) != 0, ((mt.rows >> (row0 + 8)) & 1) != 0};
+            if ((flags & 0xffffu) != 0xffffu) {
+                const bool here[2] = {((flags >> row0) & 1) != 0, ((flags >> (row0 + 8)) & 1) != 0};
 #pragma unroll
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -528,6 +548,17 @@ decode_attn_kernel(const __grid_constant__ Args a) {
             // true maxima, the lanes of a column together.
             float p[NQ][4];
             bool low = true;
+            uint2 vpar[2];
+            float vs[2][2];                      // (4-bit) scales of the two values' halves, times v_unit
+            if constexpr (F4) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    vpar[i] = *reinterpret_cast<const uint2 *>(vp8 + kTile * (G::kRow + 8) + (row0 + 8 * i) * 8);
+                    vs[i][0] = __uint_as_float(vpar[i].x << 16) * v_unit;
+                    vs[i][1] = __uint_as_float(vpar[i].y << 16) * v_unit;
+                    low = low && vs[i][0] <= kValueTop && vs[i][1] <= kValueTop;
+                }
+            }
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -536,6 +567,29 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                     low = low && p[n][e] <= 8.f;
                 }
             if (!__all_sync(0xffffffffu, low)) {
+                if constexpr (F4) {              // values far larger than any before: another unit
+                    float top = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) top = fmaxf(top, fmaxf(__uint_as_float(vpar[i].x << 16), __uint_as_float(vpar[i].y << 16)));
+#pragma unroll
+                    for (int o = 1; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    if (top * v_unit > kValueTop && top < INFINITY) {
+                        const float to = __uint_as_float((uint32_t)(127 + 100 + 127 - (int)(__float_as_uint(top) >> 23)) << 23);       // 2^(100 - exponent)
+                        const float f = to / v_unit;
+                        v_unit = to;
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                            for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) acc[n][d][e] *= f;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            vs[i][0] = __uint_as_float(vpar[i].x << 16) * v_unit;
+                            vs[i][1] = __uint_as_float(vpar[i].y << 16) * v_unit;
+                        }
+                    }
+                }
 #pragma unroll
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -563,18 +617,19 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                     l[n][e & 1] += p[n][e];
                 }
             if constexpr (F4) {
-                // sum p v = sum (p s) (c - 8) + sum p (m + 8 s), half by half: p s is the MMA's operand, rounded to bf16
+                // sum p v = sum (p s) (c - 8) + sum p (m + 8 s), half by half.  p s v_unit is the MMA's operand, rounded to bf16; a code in the
+                // last four bits of a half is the bf16 number c 2^-133 (16 c 2^-133 one nibble higher), a subnormal that needs no
+                // conversion, and -8 of all of them is one more product with the same operand.
                 uint32_t b[NQ][2][2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const uint2 pr = *reinterpret_cast<const uint2 *>(vp8 + kTile * (G::kRow + 8) + (row0 + 8 * i) * 8);
-                    const float vs[2] = {__uint_as_float(pr.x << 16), __uint_as_float(pr.y << 16)};
-                    const float mid[2] = {fmaf(8.f, vs[0], __uint_as_float(pr.x & 0xffff0000u)), fmaf(8.f, vs[1], __uint_as_float(pr.y & 0xffff0000u))};
+                    const float mid[2] = {fmaf(8.f, __uint_as_float(vpar[i].x << 16), __uint_as_float(vpar[i].x & 0xffff0000u)),
+                                          fmaf(8.f, __uint_as_float(vpar[i].y << 16), __uint_as_float(vpar[i].y & 0xffff0000u))};
 #pragma unroll
                     for (int n = 0; n < NQ; ++n)
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
-                            b[n][half][i] = transposed(pack_bf16(p[n][2 * i] * vs[half], p[n][2 * i + 1] * vs[half]));
+                            b[n][half][i] = transposed(pack_bf16(p[n][2 * i] * vs[i][half], p[n][2 * i + 1] * vs[i][half]));
 #pragma unroll
                             for (int e = 0; e < 2; ++e) off[n][half][e] = fmaf(p[n][2 * i + e], mid[half], off[n][half][e]);
                         }
@@ -599,10 +654,14 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                             for (int i = 0; i < 2; ++i) pr[jj][i] = __byte_perm(w[2 * i][x], w[2 * i + 1][x], 0x0400 + (2 * jp + jj) * 0x0101);
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
-                            const int sh = 4 * half;
-                            const uint32_t f[4] = {codes_centred(pr[0][0] >> sh), codes_centred(pr[1][0] >> sh), codes_centred(pr[0][1] >> sh), codes_centred(pr[1][1] >> sh)};
+                            const uint32_t bits = half ? 0x00f000f0u : 0x000f000fu, eight = half ? 0x80808080u : 0x80088008u;
+                            const uint32_t f[4] = {pr[0][0] & bits, pr[1][0] & bits, pr[0][1] & bits, pr[1][1] & bits}, minus[4] = {eight, eight, eight, eight};
 #pragma unroll
-                            for (int n = 0; n < NQ; ++n) mma(acc[n][(half * (D / 64) + x) * 2 + jp], f, b[n][half][0], b[n][half][1]);
+                            for (int n = 0; n < NQ; ++n) {
+                                float(&to)[4] = acc[n][(half * (D / 64) + x) * 2 + jp];
+                                mma(to, minus, b[n][half][0], b[n][half][1]);
+                                mma(to, f, b[n][half][0], b[n][half][1]);
+                            }
                         }
                     }
             } else {
@@ -621,12 +680,12 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                 }
             }
             __syncwarp();                  // all lanes are through with the stage
-            const bool ends = (mt.rows & kLast) != 0;
+            const bool ends = (flags & kLast) != 0;
             if (ends || s == my_tiles - 1) {
                 sum_up();
-                if (ends && begun_here) write_out(mt.pair);
-                else if (!begun_here) keep_part(0, part0, mt);
-                else keep_part(1, reinterpret_cast<float *>(smem + (ring - smem0)), mt);     // (nothing is on its way into the ring any more)
+                if (ends && begun_here) write_out(now.pair);
+                else if (!begun_here) keep_part(0, part0, now);
+                else keep_part(1, reinterpret_cast<float *>(smem + (ring - smem0)), now);     // (nothing is on its way into the ring any more)
             }
             at = at + 1 == G::kStages ? 0 : at + 1;
         }
@@ -639,7 +698,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
     const int first = s_first[0], last = s_first[NW];      // the block's tiles
     for (int c = 0; c <= NW; ++c) {
         const int w0 = c == 0 ? 0 : c - 1, which = c == 0 ? 0 : 1;
-        const Part pt = s_part[w0][which];
+        const Pair pt = s_part[w0][which];
         if (pt.tiles < 0) continue;
         const int end = pt.begin + pt.tiles;
         const bool here = pt.begin >= first && end <= last;
@@ -647,57 +706,73 @@ decode_attn_kernel(const __grid_constant__ Args a) {
         while (w0 + n < NW && s_first[w0 + n] < end) ++n;
         const size_t slot = 2 * (size_t)blockIdx.x + (pt.begin >= first ? 1 : 0);
         const size_t head0 = (size_t)(pt.pair / a.H_kv) * a.H_q + pt.pair % a.H_kv * a.g;
-        for (int i = tid; i < a.g * (D / 4); i += NT) {
-            const int col = i / (D / 4), el = i % (D / 4) * 4;
+        // weights of the parts, then their sums
+        if (tid < a.g) {
             float top = -INFINITY, sum = 0.f;
-            for (int w = 0; w < n; ++w) top = fmaxf(top, s_ml[w0 + w][w ? 0 : which][col].x);
+#pragma unroll
+            for (int w = 0; w < NW; ++w) top = w < n ? fmaxf(top, s_ml[w0 + w][w ? 0 : which][tid].x) : top;
             const float ref = top == -INFINITY ? 0.f : top;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int w = 0; w < n; ++w) {
-                const float2 ml = s_ml[w0 + w][w ? 0 : which][col];
-                const float f = ex2(ml.x - ref);
-                const float *src = w == 0 && which == 1 ? reinterpret_cast<const float *>(smem + w0 * G::kStages * G::kStageBytes)
-                                                        : reinterpret_cast<const float *>(smem + G::kRing) + (w0 + w) * G::kPart;
-                const float4 y = *reinterpret_cast<const float4 *>(src + col * RP + el);
-                sum = fmaf(ml.y, f, sum);
-                o.x = fmaf(y.x, f, o.x), o.y = fmaf(y.y, f, o.y), o.z = fmaf(y.z, f, o.z), o.w = fmaf(y.w, f, o.w);
-            }
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+                if (w < n) {
+                    float2 &ml = s_ml[w0 + w][w ? 0 : which][tid];
+                    ml.x = ex2(ml.x - ref);                 // the part's weight from here on
+                    sum = fmaf(ml.y, ml.x, sum);
+                }
+            s_all[tid] = make_float2(top, sum);
+        }
+        __syncthreads();
+        for (int i = tid; i < a.g * (D / 2); i += NT) {
+            const int col = i / (D / 2), el = i % (D / 2) * 2;
+            const float *src0 = which == 1 ? reinterpret_cast<const float *>(smem + w0 * G::kStages * G::kStageBytes)
+                                           : reinterpret_cast<const float *>(smem + G::kRing) + w0 * G::kPart;
+            float2 o = *reinterpret_cast<const float2 *>(src0 + col * RP + el);
+            const float f0 = s_ml[w0][which][col].x;
+            o.x *= f0, o.y *= f0;
+#pragma unroll
+            for (int w = 1; w < NW; ++w)
+                if (w < n) {
+                    const float2 y = *reinterpret_cast<const float2 *>(reinterpret_cast<const float *>(smem + G::kRing) + (w0 + w) * G::kPart + col * RP + el);
+                    const float f = s_ml[w0 + w][0][col].x;
+                    o.x = fmaf(y.x, f, o.x), o.y = fmaf(y.y, f, o.y);
+                }
+            const float top = s_all[col].x, sum = s_all[col].y;
             if (here) {
                 const float inv = top == -INFINITY ? 0.f : 1.f / sum;
-                *reinterpret_cast<uint2 *>(a.out + (head0 + col) * D + el) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+                *reinterpret_cast<uint32_t *>(a.out + (head0 + col) * D + el) = pack_bf16(o.x * inv, o.y * inv);
                 if (a.lse && el == 0) a.lse[head0 + col] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
             } else {
-                __stcg(reinterpret_cast<float4 *>(a.ws_o + (slot * kMaxGroup + col) * D + el), o);
+                __stcg(reinterpret_cast<float2 *>(a.ws_o + (slot * kMaxGroup + col) * D + el), o);
                 if (el == 0) __stcg(a.ws_ml + slot * kMaxGroup + col, make_float2(top, sum));
             }
         }
+        __syncthreads();
         if (here) continue;
-        // The pair's parts lie with the blocks b0 .. b1: worker i has the tiles from all i / workers on (rounded down), so tile x is with
-        // worker ((x + 1) workers - 1) / all.  The last of them to arrive joins them, in their order.
+        // The pair's parts lie with the blocks b0 .. b1: tile x is with worker ((x + 1) workers - 1) / all.  The last of them to arrive
+        // joins them, in their order.
         const int workers = min((int)gridDim.x * NW, all);
         const int b0 = (int)((((int64_t)pt.begin + 1) * workers - 1) / all) / NW, b1 = (int)(((int64_t)end * workers - 1) / all) / NW, n_parts = b1 - b0 + 1;
-        __syncthreads();
         if (tid == 0) {
-            __threadfence();
-            s_last = atomicInc(a.ws_count + b0, (uint32_t)(n_parts - 1)) == (uint32_t)(n_parts - 1);       // (back to 0 with the last)
-            __threadfence();
+            uint32_t before;                               // (back to 0 with the last)
+            asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(before) : "l"(a.ws_count + b0), "r"((uint32_t)(n_parts - 1)) : "memory");
+            s_last = before == (uint32_t)(n_parts - 1);
         }
         __syncthreads();
         if (s_last)
-            for (int i = tid; i < a.g * (D / 4); i += NT) {
-                const int col = i / (D / 4), el = i % (D / 4) * 4;
+            for (int i = tid; i < a.g * (D / 2); i += NT) {
+                const int col = i / (D / 2), el = i % (D / 2) * 2;
                 float top = -INFINITY, sum = 0.f;
-                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                constexpr int kBatch = 8;                       // loads in flight
+                float2 o = make_float2(0.f, 0.f);
+                constexpr int kBatch = 10;                      // loads in flight
                 for (int p0 = 0; p0 < n_parts; p0 += kBatch) {
                     float2 ml[kBatch];
-                    float4 y[kBatch];
+                    float2 y[kBatch];
 #pragma unroll
                     for (int p = 0; p < kBatch; ++p) {
                         const int i0 = min(p0 + p, n_parts - 1);
                         const size_t from = 2 * (size_t)(b0 + i0) + (i0 == 0 ? 1 : 0);
                         ml[p] = __ldcg(a.ws_ml + from * kMaxGroup + col);
-                        y[p] = __ldcg(reinterpret_cast<const float4 *>(a.ws_o + (from * kMaxGroup + col) * D + el));
+                        y[p] = __ldcg(reinterpret_cast<const float2 *>(a.ws_o + (from * kMaxGroup + col) * D + el));
                         if (p0 + p >= n_parts) ml[p] = make_float2(-INFINITY, 0.f);
                     }
                     float mx = top;
@@ -705,18 +780,18 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                     for (int p = 0; p < kBatch; ++p) mx = fmaxf(mx, ml[p].x);
                     const float ref = mx == -INFINITY ? 0.f : mx, f0 = ex2(top - ref);
                     sum *= f0;
-                    o.x *= f0, o.y *= f0, o.z *= f0, o.w *= f0;
+                    o.x *= f0, o.y *= f0;
 #pragma unroll
                     for (int p = 0; p < kBatch; ++p) {
                         if (p0 + p >= n_parts) continue;
                         const float f = ex2(ml[p].x - ref);
                         sum = fmaf(ml[p].y, f, sum);
-                        o.x = fmaf(y[p].x, f, o.x), o.y = fmaf(y[p].y, f, o.y), o.z = fmaf(y[p].z, f, o.z), o.w = fmaf(y[p].w, f, o.w);
+                        o.x = fmaf(y[p].x, f, o.x), o.y = fmaf(y[p].y, f, o.y);
                     }
                     top = mx;
                 }
                 const float inv = top == -INFINITY ? 0.f : 1.f / sum;
-                *reinterpret_cast<uint2 *>(a.out + (head0 + col) * D + el) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+                *reinterpret_cast<uint32_t *>(a.out + (head0 + col) * D + el) = pack_bf16(o.x * inv, o.y * inv);
                 if (a.lse && el == 0) a.lse[head0 + col] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
             }
     }
@@ -747,12 +822,13 @@ bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) !=
 template <int D, bool F4, int NQ>
 cudaError_t launch_decode(const Args &a, int sms, cudaStream_t st) {
     using G = Geo<D, F4, NQ>;
-    const cudaError_t e = cudaFuncSetAttribute(decode_attn_kernel<D, F4, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kBytes);
+    auto kernel = a.page_size == 8 ? decode_attn_kernel<D, F4, NQ, true> : decode_attn_kernel<D, F4, NQ, false>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kBytes);
     if (e != cudaSuccess) {
         cudaGetLastError();
         return e;
     }
-    return launch_kernel(decode_attn_kernel<D, F4, NQ>, (unsigned)sms, G::kThreads, G::kBytes, st, true, a);
+    return launch_kernel(kernel, (unsigned)sms, G::kThreads, G::kBytes, st, true, a);
 }
 
 template <bool F4>
