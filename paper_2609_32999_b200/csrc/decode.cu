@@ -40,7 +40,6 @@ int32_t api_set_error(int32_t code, const std::string &msg);
 
 namespace {
 
-constexpr int kTile = kDecodeUnit;
 constexpr float kValueUnit = 18446744073709551616.f;                 // 2^64: products with subnormal codes come out near 2^-69
 constexpr float kValueTop = 5192296858534827628530496329220096.f;    // 2^112: p (at most 2^8) times this is a bf16 number
 constexpr int kMaxGroup = 16;
@@ -58,18 +57,21 @@ struct Args {
     float2 *ws_ml;        // [2 grid][16] reference (log2 units) and sum
 };
 
-// Shared memory: every warp's ring (a stage: 16 rows of K, of V and, 4-bit, their numbers) and its part of the pair that its
-// stretch begins in; the part of the one it ends in goes into the ring.
+// Shared memory: every warp's ring (a stage: the rows of a tile of K, of V and, 4-bit, their numbers) and its part of the pair that
+// its stretch begins in; the part of the one it ends in goes into the ring.
 template <int D, bool F4, int NQ> struct Geo {
     static constexpr int kWarps = F4 && NQ == 1 ? 16 : 8;
     static constexpr int kThreads = 32 * kWarps;
+    static constexpr int kTile = F4 ? 32 : 16;                            // keys
     static constexpr int kRow = F4 ? D / 2 : 2 * D;                       // bytes of a row of K or V
     static constexpr int kStageBytes = 2 * kTile * (kRow + (F4 ? 8 : 0));
     static constexpr int kPart = 8 * NQ * (D + 4);                        // floats; rows 4 apart in banks: the lanes of a store spread over all
-    static constexpr int kStages = F4 ? (NQ == 1 ? 4 : 8) : (NQ == 1 ? 3 : 2) * (128 / D);
+    static constexpr int kStages = F4 ? (NQ == 1 ? 2 : 4) * (128 / D) : (NQ == 1 ? 3 : 2) * (128 / D);
     static constexpr int kRing = kWarps * kStages * kStageBytes;
     static constexpr int kBytes = kRing + kWarps * kPart * 4;
-    static_assert(kStages * kStageBytes >= kPart * 4, "a part goes into a warp's ring");
+    static constexpr int kChainBytes = (kWarps + 1) * 8 * NQ * 8;         // of the join, behind the part in the first warp's ring
+    static_assert(kTile % kDecodeUnit == 0, "");
+    static_assert(kStages * kStageBytes >= kPart * 4 + kChainBytes, "a part goes into a warp's ring");
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -112,169 +114,168 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// A request's visible keys: k < len with k < sinks or k >= first; its tiles: the first `front` of the request's, then those from
-// `front + skip` on, n in all.
+// A request's visible keys: k < len with k < sinks or k >= first; its tiles of T keys: the first `front` of the request's, then those
+// from `front + skip` on, n in all.
 struct Visible { int len, first, sinks, n, front, skip; };
+template <int T>
 __device__ __forceinline__ Visible visible(int len, const Args &a) {
     len = max(0, min(len, a.max_pages * a.page_size));
-    const int all = (len + kTile - 1) / kTile;
+    const int all = (len + T - 1) / T;
     if (a.window == 0 || len <= a.window) return {len, 0, 0, all, 0, 0};
-    const int first = len - a.window, sinks = min(a.n_sink, first), front = (sinks + kTile - 1) / kTile, skip = max(0, first / kTile - front);
+    const int first = len - a.window, sinks = min(a.n_sink, first), front = (sinks + T - 1) / T, skip = max(0, first / T - front);
     return {len, first, sinks, all - skip, front, skip};
 }
 
-// Where in the batch a tile lies: request, tiles of the requests before it.
-struct Start { int request, before; };
-
-// Of a stage: rows that are there (bit i: row i), and whether the tile is its pair's first and last.
-constexpr uint32_t kFirst = 1u << 30, kLast = 1u << 31;
+// Of a stage: whether the tile is its pair's first and last.
+constexpr uint32_t kFirst = 1, kLast = 2;
 
 // A pair: its number, tiles of the batch before its first, its tiles (of a warp's part: < 0, there is none).
 struct Pair { int pair, begin, tiles; };
 
-// Worker i of the batch has the tiles from all i / workers (rounded down) on; both factors of the product below 2^15.
+// Worker i of the batch has the tiles from all i / workers (rounded down) on.
 __device__ __forceinline__ int first_tile(int i, int workers, int all) {
-    if (workers == 0) return 0;
-    const uint32_t whole = (uint32_t)all / workers, rest = (uint32_t)all % workers;
-    return (int)(whole * i + rest * i / workers);
+    const uint32_t whole = (uint32_t)all / (uint32_t)workers, rest = (uint32_t)all % (uint32_t)workers;       // (rest i < 2^32: 65 536 workers)
+    return (int)(whole * (uint32_t)i + rest * (uint32_t)i / (uint32_t)workers);
+}
+// The worker of tile x: the largest i with first_tile(i) <= x.
+__device__ __forceinline__ int worker_of(int x, int workers, int all) {
+    int i = min(workers - 1, (int)((float)x * (float)workers / (float)all));           // (two too low or high at most)
+    while (first_tile(i, workers, all) > x) --i;
+    while (i + 1 < workers && first_tile(i + 1, workers, all) <= x) ++i;
+    return i;
 }
 
-// The tiles of the block's warps, [s_first[w], s_first[w + 1]), and where each begins.  Returns the number of tiles of the batch.
-// Sums run over the batch in chunks of a block's threads.  (Where there are fewer tiles than warps the first warps have one each.)
-template <int NT>
-__device__ __forceinline__ int shares(const Args &a, int *s_first, Start *s_start, int *s_sum) {
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    constexpr int W = NT / 32;
-    auto scan = [&](int x, int &total) {              // inclusive prefix sum over the block's threads
+// A warp's stretch of the batch's `all` tiles: [first, last), beginning in request r, before which lie `before` tiles.  Every warp sums the
+// batch by itself, a stretch of the requests a lane: no waiting for others, and the lengths are in L1 after the first.
+struct Stretch { int first, last, all, workers, r, before; };
+template <int T>
+__device__ __forceinline__ Stretch stretch_of(const Args &a, int worker, int most) {
+    const int lane = threadIdx.x & 31, per = (a.batch + 31) / 32, r0 = lane * per, r1 = min(a.batch, r0 + per);
+    auto tiles = [&](int r) { return a.H_kv * visible<T>(a.seq_len[r], a).n; };
+    int own = 0;
+    for (int r = r0; r < r1; ++r) own += tiles(r);
+    int end = own;
 #pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const int y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
-        }
-        if (lane == 31) s_sum[warp] = x;
-        __syncthreads();
-        int before = 0, all = 0;
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const int n = s_sum[w];
-            before += w < warp ? n : 0;
-            all += n;
-        }
-        total = all;
-        return x + before;
-    };
-    auto load = [&](int r) { return r < a.batch ? a.H_kv * visible(a.seq_len[r], a).n : 0; };
-    int own = load(tid), chunk, end = scan(own, chunk), all = chunk;
-    for (int r0 = NT; r0 < a.batch; r0 += NT) {
-        int n;
-        __syncthreads();
-        scan(load(r0 + tid), n);
-        all += n;
+    for (int o = 1; o < 32; o *= 2) {
+        const int y = __shfl_up_sync(0xffffffffu, end, o);
+        if (lane >= o) end += y;
     }
-    const int workers = min((int)gridDim.x * W, all);
-    if (tid <= W) {
-        const int i = min((int)blockIdx.x * W + tid, workers);
-        s_first[tid] = first_tile(i, workers, all);
-    }
-    __syncthreads();
-    for (int r0 = 0, before = 0; r0 < a.batch && before <= s_first[W - 1]; r0 += NT, before += chunk) {
-        if (r0 > 0) {
-            own = load(r0 + tid);
-            end = scan(own, chunk);
-        } else if (a.batch > NT) {                     // (the last chunk's sums are in the way)
-            end = scan(own, chunk);
-        }
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const int x = s_first[w] - before;
-            if (end - own <= x && x < end) s_start[w] = {r0 + tid, before + end - own};
-        }
-        if (a.batch > NT) __syncthreads();
-    }
-    __syncthreads();
-    return all;
+    Stretch s;
+    s.all = __shfl_sync(0xffffffffu, end, 31);
+    s.workers = min(most, s.all);
+    s.first = s.last = s.all;
+    s.r = s.before = 0;
+    if (worker >= s.workers) return s;                // (where there are fewer tiles than warps the first warps have one each)
+    s.first = first_tile(worker, s.workers, s.all);
+    s.last = first_tile(worker + 1, s.workers, s.all);
+    const bool mine = end - own <= s.first && s.first < end;
+    int r = r0, before = end - own;
+    if (mine)
+        for (int n = tiles(r); before + n <= s.first; n = tiles(r)) before += n, ++r;
+    const int from = __ffs(__ballot_sync(0xffffffffu, mine)) - 1;
+    s.r = __shfl_sync(0xffffffffu, r, from);
+    s.before = __shfl_sync(0xffffffffu, before, from);
+    return s;
 }
 
-template <int D, bool F4, int NQ, bool P8>
+// Requests without a key: zeros, and nothing for a sum.
+template <int D, int NT, int T>
+__device__ __forceinline__ void empty_requests(const Args &a) {
+    for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
+        if (visible<T>(a.seq_len[r], a).n == 0) {
+            for (int i = threadIdx.x; i < a.H_q * D / 8; i += NT) stg(reinterpret_cast<uint4 *>(a.out + (size_t)r * a.H_q * D) + i, make_uint4(0, 0, 0, 0));
+            if (a.lse)
+                for (int i = threadIdx.x; i < a.H_q; i += NT) a.lse[(size_t)r * a.H_q + i] = -INFINITY;
+        }
+}
+
+// SMALL: pages of fewer tokens than a tile.
+template <int D, bool F4, int NQ, bool SMALL>
 __global__ void __launch_bounds__(Geo<D, F4, NQ>::kThreads, 1)
 decode_attn_kernel(const __grid_constant__ Args a) {
     using G = Geo<D, F4, NQ>;
-    constexpr int NW = G::kWarps, NT = G::kThreads, CPR = G::kRow / 16, Q8 = 8 * NQ, KS = D / 16, RP = D + 4;
+    constexpr int T = G::kTile, SUB = T / 16, NW = G::kWarps, NT = G::kThreads, CPR = G::kRow / 16, Q8 = 8 * NQ, KS = D / 16, RP = D + 4;
+    constexpr uint32_t kAllRows = T == 32 ? 0xffffffffu : 0xffffu;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ uint32_t s_flags[NW][G::kStages];
+    __shared__ uint2 s_stage[NW][G::kStages];         // rows that are there (bit i: row i) and flags
     __shared__ Pair s_pair[NW][G::kStages];           // of a stage that is its pair's first, or the warp's
     __shared__ float2 s_ml[NW][2][Q8];
-    __shared__ float2 s_all[Q8];                      // reference and sum of a chain
     __shared__ Pair s_part[NW][2];                    // [0]: of a pair that began before the warp's stretch, [1]: of one that goes on behind it
-    __shared__ Start s_start[NW];
-    __shared__ int s_first[NW + 1], s_sum[NW], s_last;
+    __shared__ int s_first[NW + 1], s_length[NW + 1], s_leaves[2], s_join[2][2];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, quad = lane / 4, t = lane % 4;
     const int page_shift = __ffs(a.page_size) - 1;
     if (lane < 2) s_part[warp][lane] = {0, 0, -1};
+    if (tid < 2) s_leaves[tid] = -1;
     grid_wait();
     grid_release();
-    const int all = shares<NT>(a, s_first, s_start, s_sum);
-    const int my_tiles = s_first[warp + 1] - s_first[warp];
+    const Stretch mine = stretch_of<T>(a, (int)blockIdx.x * NW + warp, (int)gridDim.x * NW);
+    if (lane == 0) {
+        s_first[warp] = mine.first;
+        if (warp == NW - 1) s_first[NW] = mine.last;
+    }
+    const int my_tiles = mine.last - mine.first;
     const uint32_t smem0 = ptx::smem_u32(smem), ring = smem0 + warp * G::kStages * G::kStageBytes;
     float *part0 = reinterpret_cast<float *>(smem + G::kRing) + warp * G::kPart;
 
     if (my_tiles > 0) {
-        // ---- the warp's fetching end: where the next tile to be sent for lies, and the page ids of 32 tiles from jb on, one a lane
-        // (P8: pages of 8 tokens, two a tile)
-        int r = s_start[warp].request, base = s_start[warp].before, sent = 0, h, j, jb, page_a, page_b = 0;
-        Visible vis = visible(a.seq_len[r], a);
-        h = (s_first[warp] - base) / vis.n;
-        j = jb = (s_first[warp] - base) - h * vis.n;
+        // ---- the warp's fetching end: where the next tile to be sent for lies, and the page ids of the next kBatch tiles from jb on,
+        // one a lane (SMALL: one a lane for every 8 rows)
+        constexpr int GROUPS = T / 8, kBatch = SMALL ? 32 / GROUPS : 32;
+        int r = mine.r, base = mine.before, sent = 0, h, j, jb, page_ids;
+        Visible vis = visible<T>(a.seq_len[r], a);
+        h = (mine.first - base) / vis.n;
+        j = jb = (mine.first - base) - h * vis.n;
         auto tile_at = [&](int i) { return i < vis.front ? i : i + vis.skip; };
         auto load_pages = [&]() {
-            const int32_t *table = a.table + (size_t)r * a.max_pages;
-            const int i = jb + lane, key0 = tile_at(i) * kTile;
-            page_a = i < vis.n ? table[key0 >> page_shift] : -1;
-            if (P8) page_b = i < vis.n && key0 + 8 < vis.len ? table[(key0 >> page_shift) + 1] : -1;
+            const int i = jb + (SMALL ? lane / GROUPS : lane), key = tile_at(i) * T + (SMALL ? lane % GROUPS * 8 : 0);
+            page_ids = i < vis.n && key < vis.len ? a.table[(size_t)r * a.max_pages + (key >> page_shift)] : -1;
         };
         load_pages();
-        // A lane's own places: of its 16 bytes of the rows (and its 8 of their numbers) in page 0 of head h.
+        // A lane's own places: of its 16 bytes of the rows (and its 8 of their numbers) in page 0 of head 0.
         constexpr int RPT = 32 / CPR;              // rows a turn of 32 lanes
         const uint32_t head_bytes = F4 ? (uint32_t)a.page_size * (D / 2 + 8) : (uint32_t)G::kRow;
         const uint32_t row_bytes = F4 ? (uint32_t)G::kRow : a.H_kv * head_bytes, page_bytes = F4 ? a.H_kv * head_bytes : row_bytes << page_shift;
-        const uint32_t place = (lane / CPR) * row_bytes + lane % CPR * 16;
-        const uint32_t place4 = (uint32_t)a.page_size * (D / 2) + (lane & 15) * 8;
+        const uint32_t numbers = (uint32_t)a.page_size * (D / 2);
         auto fetch = [&](int at) {
             if (sent < my_tiles) {
-                const int key0 = tile_at(j) * kTile, off = key0 & (a.page_size - 1), pa = __shfl_sync(0xffffffffu, page_a, j - jb);
-                const int pb = P8 ? __shfl_sync(0xffffffffu, page_b, j - jb) : pa;
+                const int key0 = tile_at(j) * T;
                 auto in_pool = [&](int page) { return (uint32_t)page < (uint32_t)a.num_pool_pages; };
-                uint32_t rows = 0xffffu;
-                if (!(in_pool(pa) && (!P8 || in_pool(pb)) && key0 + kTile <= vis.len && (key0 >= vis.first || key0 + kTile <= vis.sinks))) {
-                    const int key = key0 + (lane & 15);
-                    rows = __ballot_sync(0xffffffffu, key < vis.len && (key < vis.sinks || key >= vis.first) && in_pool(lane & 8 ? pb : pa)) & 0xffffu;
+                // the page of row `row` (of any where a page holds the tile)
+                auto page_of = [&](int row) { return __shfl_sync(0xffffffffu, page_ids, SMALL ? (j - jb) * GROUPS + row / 8 : j - jb); };
+                const int page = page_of(lane & (T - 1));
+                uint32_t rows = kAllRows;
+                if (SMALL || !(in_pool(page) && key0 + T <= vis.len && (key0 >= vis.first || key0 + T <= vis.sinks))) {
+                    const int key = key0 + (lane & (T - 1));
+                    rows = __ballot_sync(0xffffffffu, key < vis.len && (key < vis.sinks || key >= vis.first) && in_pool(page)) & kAllRows;
                 }
-                if (lane == 0) s_flags[warp][at] = rows | (j == 0 ? kFirst : 0u) | (j == vis.n - 1 ? kLast : 0u);
-                if ((j == 0 || sent == 0) && lane == 0) s_pair[warp][at] = {r * a.H_kv + h, base + h * vis.n, vis.n};
-                const uint32_t kb = ring + at * G::kStageBytes, vb = kb + kTile * G::kRow;
+                if (lane == 0) {
+                    s_stage[warp][at] = make_uint2(rows, (j == 0 ? kFirst : 0u) | (j == vis.n - 1 ? kLast : 0u));
+                    if (j == 0 || sent == 0) s_pair[warp][at] = {r * a.H_kv + h, base + h * vis.n, vis.n};
+                }
+                const uint32_t kb = ring + at * G::kStageBytes, vb = kb + T * G::kRow;
                 auto copy = [&](auto all_there) {
                     constexpr bool ALL = decltype(all_there)::value;
                     // (of a page that is not there nothing is read)
-                    const uint64_t p0 = (uint64_t)(ALL || in_pool(pa) ? (uint32_t)pa : 0u) * page_bytes + h * head_bytes + off * (uint64_t)row_bytes + place;
-                    const uint64_t p1 = P8 ? (uint64_t)(ALL || in_pool(pb) ? (uint32_t)pb : 0u) * page_bytes + h * head_bytes + place : p0 + 8 * (uint64_t)row_bytes;
+                    auto page_at = [&](int id) { return (uint64_t)(ALL || in_pool(id) ? (uint32_t)id : 0u) * page_bytes + h * head_bytes; };
+                    const uint64_t p0 = page_at(page) + (key0 & (a.page_size - 1)) * (uint64_t)row_bytes + lane / CPR * row_bytes + lane % CPR * 16;
 #pragma unroll
-                    for (int i = 0; i < kTile / RPT; ++i) {
+                    for (int i = 0; i < T / RPT; ++i) {
                         const int row = i * RPT + lane / CPR, c = lane % CPR;
-                        // a lane's rows of this turn: all in one half of the tile, but where a turn is the whole tile
-                        const uint64_t o = RPT == 16 ? (lane < 16 || !P8 ? p0 : p1 - 8 * (uint64_t)row_bytes) : i * RPT < 8 ? p0 + (uint64_t)(i * RPT) * row_bytes : p1 + (uint64_t)(i * RPT - 8) * row_bytes;
+                        uint64_t o = p0 + (uint64_t)(i * RPT) * row_bytes;
+                        if constexpr (SMALL) o = page_at(page_of(row)) + ((key0 + row) & (a.page_size - 1)) * (uint64_t)row_bytes + c * 16;
                         // 16-bit: chunks turned by the row, as ldmatrix wants them; 4-bit values: the halves of rows 4-7 of 8 change places, so
                         // that the four rows and eight columns that a warp's lanes ask for at once lie in different banks
                         const int ck = F4 ? c : c ^ (row & 7), cv = F4 ? (D == 128 ? c ^ (((row >> 2) & 1) << 1) : c) : ck;
                         cp_async<16, ALL>(kb + row * G::kRow + ck * 16, a.k + o, (rows >> row) & 1);
                         cp_async<16, ALL>(vb + row * G::kRow + cv * 16, a.v + o, (rows >> row) & 1);
                     }
-                    if constexpr (F4) {
-                        const bool second = P8 && (lane & 8);
-                        const uint64_t o = (uint64_t)(ALL || in_pool(second ? pb : pa) ? (uint32_t)(second ? pb : pa) : 0u) * page_bytes + h * head_bytes + (second ? -64 : off * 8) + place4;
-                        cp_async<8, ALL>(vb + kTile * G::kRow + lane * 8, (lane < 16 ? a.k : a.v) + o, (rows >> (lane & 15)) & 1);
+                    if constexpr (F4) {                 // (T = 32: a lane has a row's numbers, and the row's page)
+                        const uint64_t o = page_at(page) + numbers + (SMALL ? (key0 + lane) & (a.page_size - 1) : (key0 & (a.page_size - 1)) + lane) * 8;
+                        cp_async<8, ALL>(vb + T * G::kRow + lane * 8, a.k + o, (rows >> lane) & 1);
+                        cp_async<8, ALL>(vb + T * G::kRow + T * 8 + lane * 8, a.v + o, (rows >> lane) & 1);
                     }
                 };
-                if (rows == 0xffffu) copy(std::true_type{});
+                if (rows == kAllRows) copy(std::true_type{});
                 else copy(std::false_type{});
                 if (++sent < my_tiles) {
                     if (++j == vis.n) {
@@ -284,11 +285,11 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                             h = 0;
                             do {
                                 base += vis.n * a.H_kv;
-                                vis = visible(a.seq_len[++r], a);
+                                vis = visible<T>(a.seq_len[++r], a);
                             } while (vis.n == 0);
                         }
                         if (!same) load_pages();
-                    } else if (j - jb == 32) {
+                    } else if (j - jb == kBatch) {
                         jb = j;
                         load_pages();
                     }
@@ -470,107 +471,112 @@ decode_attn_kernel(const __grid_constant__ Args a) {
             cp_wait<G::kStages - 2>();
             __syncwarp();
             fetch(at == 0 ? G::kStages - 1 : at - 1);      // into the stage consumed in the last turn
-            const uint32_t flags = s_flags[warp][at];
-            if (s == 0 || (flags & kFirst)) {
+            const uint2 stage = s_stage[warp][at];
+            if (s == 0 || (stage.y & kFirst)) {
                 now = s_pair[warp][at];
-                begun_here = (flags & kFirst) != 0;
+                begun_here = (stage.y & kFirst) != 0;
                 if (s > 0) begin_pair(now.pair);
             }
-            const uint32_t kb = ring + at * G::kStageBytes, vb = kb + kTile * G::kRow;
+            const uint32_t kb = ring + at * G::kStageBytes, vb = kb + T * G::kRow;
             const uint8_t *kp8 = smem + (kb - smem0), *vp8 = smem + (vb - smem0);
-            // rows of the score tile: natural keys of the 16, 4-bit: row i is key i ^ (i / 2 % 2) (see the bank note above)
+            // rows of a score tile: natural keys of the 16, 4-bit: row i is key i ^ (i / 2 % 2) (see the bank note above)
             const int row0 = F4 ? quad ^ ((quad >> 1) & 1) : quad;
-            float sc[NQ][4];
-            if constexpr (F4) {
-                float part[NQ][2][4];
+            float sc[SUB][NQ][4];
 #pragma unroll
-                for (int n = 0; n < NQ; ++n)
+            for (int sub = 0; sub < SUB; ++sub)
+                if constexpr (F4) {
+                    float part[NQ][2][4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) part[n][0][e] = part[n][1][e] = 0.f;
-                uint32_t w[2][D / 32];               // 16 (8) bytes of rows row0 and row0 + 8
-                float par[2][4];                     // their scales and least values
+                    for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint8_t *p = kp8 + (row0 + 8 * i) * G::kRow + (D / 8) * t;
-                    if constexpr (D == 128) *reinterpret_cast<uint4 *>(w[i]) = *reinterpret_cast<const uint4 *>(p);
-                    else *reinterpret_cast<uint2 *>(w[i]) = *reinterpret_cast<const uint2 *>(p);
-                    const uint2 pr = *reinterpret_cast<const uint2 *>(vp8 + kTile * G::kRow + (row0 + 8 * i) * 8);
-                    par[i][0] = __uint_as_float(pr.x << 16), par[i][1] = __uint_as_float(pr.x & 0xffff0000u);
-                    par[i][2] = __uint_as_float(pr.y << 16), par[i][3] = __uint_as_float(pr.y & 0xffff0000u);
-                }
+                        for (int e = 0; e < 4; ++e) part[n][0][e] = part[n][1][e] = 0.f;
+                    uint32_t w[2][D / 32];               // 16 (8) bytes of rows row0 and row0 + 8
 #pragma unroll
-                for (int x = 0; x < D / 32; ++x) {
-                    const uint32_t w0 = w[0][x], w1 = w[1][x], u0 = w0 >> 8, u1 = w1 >> 8;
-                    const uint32_t lo[4] = {w0 & 0x000f000fu, w1 & 0x000f000fu, u0 & 0x000f000fu, u1 & 0x000f000fu};
-                    const uint32_t hi[4] = {w0 & 0x00f000f0u, w1 & 0x00f000f0u, u0 & 0x00f000f0u, u1 & 0x00f000f0u};
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) {
-                        mma_f16(part[n][0], lo, qf[n][x][0], qf[n][x][1]);
-                        mma_f16(part[n][1], hi, qf[n][KS / 2 + x][0], qf[n][KS / 2 + x][1]);
+                    for (int i = 0; i < 2; ++i) {
+                        const uint8_t *b = kp8 + (sub * 16 + row0 + 8 * i) * G::kRow + (D / 8) * t;
+                        if constexpr (D == 128) *reinterpret_cast<uint4 *>(w[i]) = *reinterpret_cast<const uint4 *>(b);
+                        else *reinterpret_cast<uint2 *>(w[i]) = *reinterpret_cast<const uint2 *>(b);
                     }
+#pragma unroll
+                    for (int x = 0; x < D / 32; ++x) {
+                        const uint32_t w0 = w[0][x], w1 = w[1][x], u0 = w0 >> 8, u1 = w1 >> 8;
+                        const uint32_t lo[4] = {w0 & 0x000f000fu, w1 & 0x000f000fu, u0 & 0x000f000fu, u1 & 0x000f000fu};
+                        const uint32_t hi[4] = {w0 & 0x00f000f0u, w1 & 0x00f000f0u, u0 & 0x00f000f0u, u1 & 0x00f000f0u};
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) {
+                            mma_f16(part[n][0], lo, qf[n][x][0], qf[n][x][1]);
+                            mma_f16(part[n][1], hi, qf[n][KS / 2 + x][0], qf[n][KS / 2 + x][1]);
+                        }
+                    }
+                    // q.k = sum over the halves of s (q.c) + m sum q
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint2 pr = *reinterpret_cast<const uint2 *>(vp8 + T * G::kRow + (sub * 16 + row0 + 8 * i) * 8);
+                        const float s0 = __uint_as_float(pr.x << 16), m0 = __uint_as_float(pr.x & 0xffff0000u), s1 = __uint_as_float(pr.y << 16), m1 = __uint_as_float(pr.y & 0xffff0000u);
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                sc[sub][n][2 * i + e] = fmaf(s0, part[n][0][2 * i + e], fmaf(m0, q_sum[n][0][e], fmaf(s1, part[n][1][2 * i + e], m1 * q_sum[n][1][e])));
+                    }
+                } else {
+                    float odd[NQ][4];                    // (two chains of products)
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[sub][n][e] = odd[n][e] = 0.f;
+                    const int lr = sub * 16 + (lane & 15);            // lanes 0-15: rows, first 8 columns; 16-31: next 8
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) {
+                        uint32_t f[4];
+                        ldmatrix_x4(f, kb + lr * G::kRow + (((2 * ks + (lane >> 4)) ^ (lr & 7)) << 4));
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) mma(ks & 1 ? odd[n] : sc[sub][n], f, qf[n][ks][0], qf[n][ks][1]);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[sub][n][e] += odd[n][e];
                 }
-                // q.k = sum over the halves of s (q.c) + m sum q
+            if (stage.x != kAllRows) {
+#pragma unroll
+                for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!((stage.x >> (sub * 16 + row0 + 8 * (e >> 1))) & 1)) sc[sub][n][e] = a.scale_log2 < 0.f ? INFINITY : -INFINITY;
+            }
+            // Weights against the reference; that moves only where a score would go far above it (and at the first keys): then to the
+            // columns' true maxima, the lanes of a column together.
+            float p[SUB][NQ][4];
+            bool low = true;
+            uint2 vpar[SUB][2];                  // (4-bit) the values' numbers
+            if constexpr (F4) {
+#pragma unroll
+                for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        vpar[sub][i] = *reinterpret_cast<const uint2 *>(vp8 + T * (G::kRow + 8) + (sub * 16 + row0 + 8 * i) * 8);
+                        low = low && __uint_as_float(vpar[sub][i].x << 16) * v_unit <= kValueTop && __uint_as_float(vpar[sub][i].y << 16) * v_unit <= kValueTop;
+                    }
+            }
+#pragma unroll
+            for (int sub = 0; sub < SUB; ++sub)
 #pragma unroll
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int i = e >> 1;
-                        sc[n][e] = fmaf(par[i][0], part[n][0][e], fmaf(par[i][1], q_sum[n][0][e & 1], fmaf(par[i][2], part[n][1][e], par[i][3] * q_sum[n][1][e & 1])));
+                        p[sub][n][e] = fmaf(sc[sub][n][e], unit[n][e & 1], -m[n][e & 1]);
+                        low = low && p[sub][n][e] <= 8.f;
                     }
-            } else {
-                float odd[NQ][4];                    // (two chains of products)
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[n][e] = odd[n][e] = 0.f;
-                const int lr = lane & 15;            // lanes 0-15: rows, first 8 columns; 16-31: next 8
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    uint32_t f[4];
-                    ldmatrix_x4(f, kb + lr * G::kRow + (((2 * ks + (lane >> 4)) ^ (lr & 7)) << 4));
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) mma(ks & 1 ? odd[n] : sc[n], f, qf[n][ks][0], qf[n][ks][1]);
-                }
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[n][e] += odd[n][e];
-            }
-            if ((flags & 0xffffu) != 0xffffu) {
-                const bool here[2] = {((flags >> row0) & 1) != 0, ((flags >> (row0 + 8)) & 1) != 0};
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!here[e >> 1]) sc[n][e] = a.scale_log2 < 0.f ? INFINITY : -INFINITY;
-            }
-            // p against the reference; that moves only where a score would go far above it (and at the first keys): then to the columns'
-            // true maxima, the lanes of a column together.
-            float p[NQ][4];
-            bool low = true;
-            uint2 vpar[2];
-            float vs[2][2];                      // (4-bit) scales of the two values' halves, times v_unit
-            if constexpr (F4) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    vpar[i] = *reinterpret_cast<const uint2 *>(vp8 + kTile * (G::kRow + 8) + (row0 + 8 * i) * 8);
-                    vs[i][0] = __uint_as_float(vpar[i].x << 16) * v_unit;
-                    vs[i][1] = __uint_as_float(vpar[i].y << 16) * v_unit;
-                    low = low && vs[i][0] <= kValueTop && vs[i][1] <= kValueTop;
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[n][e] = fmaf(sc[n][e], unit[n][e & 1], -m[n][e & 1]);
-                    low = low && p[n][e] <= 8.f;
-                }
             if (!__all_sync(0xffffffffu, low)) {
                 if constexpr (F4) {              // values far larger than any before: another unit
                     float top = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) top = fmaxf(top, fmaxf(__uint_as_float(vpar[i].x << 16), __uint_as_float(vpar[i].y << 16)));
+                    for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) top = fmaxf(top, fmaxf(__uint_as_float(vpar[sub][i].x << 16), __uint_as_float(vpar[sub][i].y << 16)));
 #pragma unroll
                     for (int o = 1; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                     if (top * v_unit > kValueTop && top < INFINITY) {
@@ -583,18 +589,15 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                             for (int d = 0; d < D / 16; ++d)
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) acc[n][d][e] *= f;
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            vs[i][0] = __uint_as_float(vpar[i].x << 16) * v_unit;
-                            vs[i][1] = __uint_as_float(vpar[i].y << 16) * v_unit;
-                        }
                     }
                 }
 #pragma unroll
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float top = fmaxf(sc[n][e] * unit[n][e], sc[n][e + 2] * unit[n][e]);
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int sub = 0; sub < SUB; ++sub) top = fmaxf(top, fmaxf(sc[sub][n][e] * unit[n][e], sc[sub][n][e + 2] * unit[n][e]));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
@@ -606,81 +609,88 @@ decode_attn_kernel(const __grid_constant__ Args a) {
 #pragma unroll
                         for (int d = 0; d < D / 16; ++d) acc[n][d][e] *= f, acc[n][d][e + 2] *= f;
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) p[n][e + 2 * i] = fmaf(sc[n][e + 2 * i], unit[n][e], -ref);
+                        for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) p[sub][n][e + 2 * i] = fmaf(sc[sub][n][e + 2 * i], unit[n][e], -ref);
                     }
             }
 #pragma unroll
-            for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[n][e] = ex2(p[n][e]);
-                    l[n][e & 1] += p[n][e];
-                }
-            if constexpr (F4) {
-                // sum p v = sum (p s) (c - 8) + sum p (m + 8 s), half by half.  p s v_unit is the MMA's operand, rounded to bf16; a code in the
-                // last four bits of a half is the bf16 number c 2^-133 (16 c 2^-133 one nibble higher), a subnormal that needs no
-                // conversion, and -8 of all of them is one more product with the same operand.
-                uint32_t b[NQ][2][2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float mid[2] = {fmaf(8.f, __uint_as_float(vpar[i].x << 16), __uint_as_float(vpar[i].x & 0xffff0000u)),
-                                          fmaf(8.f, __uint_as_float(vpar[i].y << 16), __uint_as_float(vpar[i].y & 0xffff0000u))};
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            b[n][half][i] = transposed(pack_bf16(p[n][2 * i] * vs[i][half], p[n][2 * i + 1] * vs[i][half]));
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) off[n][half][e] = fmaf(p[n][2 * i + e], mid[half], off[n][half][e]);
-                        }
-                }
-                // keys of operand rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9, and of each the bytes whose elements this lane's rows of V^T are
-                uint32_t w[4][D / 64];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int op = 2 * t + (i & 1), row = (i >> 1) * 8 + (op ^ ((op >> 1) & 1));
-                    const uint8_t *p8 = vp8 + row * G::kRow;
-                    if constexpr (D == 128) *reinterpret_cast<uint2 *>(w[i]) = *reinterpret_cast<const uint2 *>(p8 + ((quad * 8) ^ (((row >> 2) & 1) << 5)));
-                    else w[i][0] = *reinterpret_cast<const uint32_t *>(p8 + quad * 4);
-                }
-#pragma unroll
-                for (int x = 0; x < D / 64; ++x)
-#pragma unroll
-                    for (int jp = 0; jp < 2; ++jp) {
-                        uint32_t pr[2][2];                // byte 2 jp + j of two keys, operand rows 2 i and 2 i + 1 of the four
-#pragma unroll
-                        for (int jj = 0; jj < 2; ++jj)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) pr[jj][i] = __byte_perm(w[2 * i][x], w[2 * i + 1][x], 0x0400 + (2 * jp + jj) * 0x0101);
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const uint32_t bits = half ? 0x00f000f0u : 0x000f000fu, eight = half ? 0x80808080u : 0x80088008u;
-                            const uint32_t f[4] = {pr[0][0] & bits, pr[1][0] & bits, pr[0][1] & bits, pr[1][1] & bits}, minus[4] = {eight, eight, eight, eight};
-#pragma unroll
-                            for (int n = 0; n < NQ; ++n) {
-                                float(&to)[4] = acc[n][(half * (D / 64) + x) * 2 + jp];
-                                mma(to, minus, b[n][half][0], b[n][half][1]);
-                                mma(to, f, b[n][half][0], b[n][half][1]);
-                            }
-                        }
-                    }
-            } else {
-                uint32_t b[NQ][2];
+            for (int sub = 0; sub < SUB; ++sub) {
 #pragma unroll
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) b[n][i] = transposed(pack_bf16(p[n][2 * i], p[n][2 * i + 1]));
-                const int lr = (lane & 7) + ((lane >> 4) << 3), lc = (lane >> 3) & 1;      // blocks: keys 0-7 | 8-15 by lanes 0-15 | 16-31, columns alternating
+                    for (int e = 0; e < 4; ++e) {
+                        p[sub][n][e] = ex2(p[sub][n][e]);
+                        l[n][e & 1] += p[sub][n][e];
+                    }
+                if constexpr (F4) {
+                    // sum p v = sum (p s) (c - 8) + sum p (m + 8 s), half by half.  p s v_unit is the MMA's operand, rounded to bf16; a code in the
+                    // last four bits of a half is the bf16 number c 2^-133 (16 c 2^-133 one nibble higher), a subnormal that needs no
+                    // conversion, and -8 of all of them is one more product with the same operand.
+                    uint32_t b[NQ][2][2];
 #pragma unroll
-                for (int d = 0; d < D / 16; ++d) {
-                    uint32_t f[4];
-                    ldmatrix_x4_trans(f, vb + lr * G::kRow + (((2 * d + lc) ^ (lr & 7)) << 4));
+                    for (int i = 0; i < 2; ++i) {
+                        const float vs[2] = {__uint_as_float(vpar[sub][i].x << 16), __uint_as_float(vpar[sub][i].y << 16)};
+                        const float mid[2] = {fmaf(8.f, vs[0], __uint_as_float(vpar[sub][i].x & 0xffff0000u)), fmaf(8.f, vs[1], __uint_as_float(vpar[sub][i].y & 0xffff0000u))};
 #pragma unroll
-                    for (int n = 0; n < NQ; ++n) mma(acc[n][d], f, b[n][0], b[n][1]);
+                        for (int half = 0; half < 2; ++half) {
+                            const float su = vs[half] * v_unit;
+#pragma unroll
+                            for (int n = 0; n < NQ; ++n) {
+                                b[n][half][i] = transposed(pack_bf16(p[sub][n][2 * i] * su, p[sub][n][2 * i + 1] * su));
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) off[n][half][e] = fmaf(p[sub][n][2 * i + e], mid[half], off[n][half][e]);
+                            }
+                        }
+                    }
+                    // keys of operand rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9, and of each the bytes whose elements this lane's rows of V^T are
+                    uint32_t w[4][D / 64];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int op = 2 * t + (i & 1), row = sub * 16 + (i >> 1) * 8 + (op ^ ((op >> 1) & 1));
+                        const uint8_t *p8 = vp8 + row * G::kRow;
+                        if constexpr (D == 128) *reinterpret_cast<uint2 *>(w[i]) = *reinterpret_cast<const uint2 *>(p8 + ((quad * 8) ^ (((row >> 2) & 1) << 5)));
+                        else w[i][0] = *reinterpret_cast<const uint32_t *>(p8 + quad * 4);
+                    }
+#pragma unroll
+                    for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+                        for (int jp = 0; jp < 2; ++jp) {
+                            uint32_t pr[2][2];                // byte 2 jp + j of two keys, operand rows 2 i and 2 i + 1 of the four
+#pragma unroll
+                            for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) pr[jj][i] = __byte_perm(w[2 * i][x], w[2 * i + 1][x], 0x0400 + (2 * jp + jj) * 0x0101);
+#pragma unroll
+                            for (int half = 0; half < 2; ++half) {
+                                const uint32_t bits = half ? 0x00f000f0u : 0x000f000fu, eight = half ? 0x80808080u : 0x80088008u;
+                                const uint32_t f[4] = {pr[0][0] & bits, pr[1][0] & bits, pr[0][1] & bits, pr[1][1] & bits}, minus[4] = {eight, eight, eight, eight};
+#pragma unroll
+                                for (int n = 0; n < NQ; ++n) {
+                                    float(&to)[4] = acc[n][(half * (D / 64) + x) * 2 + jp];
+                                    mma(to, minus, b[n][half][0], b[n][half][1]);
+                                    mma(to, f, b[n][half][0], b[n][half][1]);
+                                }
+                            }
+                        }
+                } else {
+                    uint32_t b[NQ][2];
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) b[n][i] = transposed(pack_bf16(p[sub][n][2 * i], p[sub][n][2 * i + 1]));
+                    const int lr = sub * 16 + (lane & 7) + ((lane >> 4) << 3), lc = (lane >> 3) & 1;      // blocks: keys 0-7 | 8-15 by lanes 0-15 | 16-31, columns alternating
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d) {
+                        uint32_t f[4];
+                        ldmatrix_x4_trans(f, vb + lr * G::kRow + (((2 * d + lc) ^ (lr & 7)) << 4));
+#pragma unroll
+                        for (int n = 0; n < NQ; ++n) mma(acc[n][d], f, b[n][0], b[n][1]);
+                    }
                 }
             }
             __syncwarp();                  // all lanes are through with the stage
-            const bool ends = (flags & kLast) != 0;
+            const bool ends = (stage.y & kLast) != 0;
             if (ends || s == my_tiles - 1) {
                 sum_up();
                 if (ends && begun_here) write_out(now.pair);
@@ -693,35 +703,47 @@ decode_attn_kernel(const __grid_constant__ Args a) {
     }
     __syncthreads();
 
-    // ---- the block's parts.  A chain is one pair's: a part at a stretch's end (or, of a pair that began before the block, at the
-    // first stretch's beginning), then the following warps' parts at their beginnings.
+    // ---- the block's parts.  A chain is one pair's: a part at a stretch's end (c - 1 is the warp; or, c = 0, of a pair that began before
+    // the block, at the first stretch's beginning), then the following warps' parts at their beginnings.
     const int first = s_first[0], last = s_first[NW];      // the block's tiles
-    for (int c = 0; c <= NW; ++c) {
-        const int w0 = c == 0 ? 0 : c - 1, which = c == 0 ? 0 : 1;
+    float2 *s_chain = reinterpret_cast<float2 *>(smem + G::kPart * 4);        // [NW + 1][Q8] reference and sum of a chain
+    for (int i = tid; i < (NW + 1) * Q8; i += NT) {
+        const int c = i / Q8, col = i % Q8, w0 = max(c - 1, 0), which = c == 0 ? 0 : 1;
         const Pair pt = s_part[w0][which];
-        if (pt.tiles < 0) continue;
-        const int end = pt.begin + pt.tiles;
-        const bool here = pt.begin >= first && end <= last;
-        int n = 1;                                          // warps with a part of it
-        while (w0 + n < NW && s_first[w0 + n] < end) ++n;
-        const size_t slot = 2 * (size_t)blockIdx.x + (pt.begin >= first ? 1 : 0);
-        const size_t head0 = (size_t)(pt.pair / a.H_kv) * a.H_q + pt.pair % a.H_kv * a.g;
-        // weights of the parts, then their sums
-        if (tid < a.g) {
-            float top = -INFINITY, sum = 0.f;
+        int n = 0;                                          // warps with a part of it
+        if (pt.tiles >= 0) {
+            const int end = pt.begin + pt.tiles;
+            n = 1;
+            float2 ml[NW];                                  // (all loads at once)
 #pragma unroll
-            for (int w = 0; w < NW; ++w) top = w < n ? fmaxf(top, s_ml[w0 + w][w ? 0 : which][tid].x) : top;
+            for (int w = 1; w < NW; ++w) n += w > w0 && s_first[w] < end;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) ml[w] = s_ml[min(w0 + w, NW - 1)][w ? 0 : which][col];
+            float top = ml[0].x;
+#pragma unroll
+            for (int w = 1; w < NW; ++w) top = w < n ? fmaxf(top, ml[w].x) : top;
             const float ref = top == -INFINITY ? 0.f : top;
+            float sum = 0.f;
 #pragma unroll
             for (int w = 0; w < NW; ++w)
                 if (w < n) {
-                    float2 &ml = s_ml[w0 + w][w ? 0 : which][tid];
-                    ml.x = ex2(ml.x - ref);                 // the part's weight from here on
-                    sum = fmaf(ml.y, ml.x, sum);
+                    const float f = ex2(ml[w].x - ref);
+                    s_ml[w0 + w][w ? 0 : which][col].x = f;              // the part's weight from here on
+                    sum = fmaf(ml[w].y, f, sum);
                 }
-            s_all[tid] = make_float2(top, sum);
+            s_chain[c * Q8 + col] = make_float2(top, sum);
+            if (col == 0 && !(pt.begin >= first && end <= last)) s_leaves[pt.begin >= first ? 1 : 0] = c;
         }
-        __syncthreads();
+        if (col == 0) s_length[c] = n;
+    }
+    __syncthreads();
+    for (uint32_t left = __ballot_sync(0xffffffffu, lane <= NW && s_length[min(lane, NW)] > 0); left; left &= left - 1) {
+        const int c = __ffs(left) - 1, n = s_length[c];
+        const int w0 = max(c - 1, 0), which = c == 0 ? 0 : 1;
+        const Pair pt = s_part[w0][which];
+        const bool here = pt.begin >= first && pt.begin + pt.tiles <= last;
+        const size_t slot = 2 * (size_t)blockIdx.x + (pt.begin >= first ? 1 : 0);
+        const size_t head0 = (size_t)(pt.pair / a.H_kv) * a.H_q + pt.pair % a.H_kv * a.g;
         for (int i = tid; i < a.g * (D / 2); i += NT) {
             const int col = i / (D / 2), el = i % (D / 2) * 2;
             const float *src0 = which == 1 ? reinterpret_cast<const float *>(smem + w0 * G::kStages * G::kStageBytes)
@@ -729,80 +751,88 @@ decode_attn_kernel(const __grid_constant__ Args a) {
             float2 o = *reinterpret_cast<const float2 *>(src0 + col * RP + el);
             const float f0 = s_ml[w0][which][col].x;
             o.x *= f0, o.y *= f0;
+            for (int w1 = 1; w1 < n; w1 += 4) {
+                float2 y[4];
+                float f[4];
 #pragma unroll
-            for (int w = 1; w < NW; ++w)
-                if (w < n) {
-                    const float2 y = *reinterpret_cast<const float2 *>(reinterpret_cast<const float *>(smem + G::kRing) + (w0 + w) * G::kPart + col * RP + el);
-                    const float f = s_ml[w0 + w][0][col].x;
-                    o.x = fmaf(y.x, f, o.x), o.y = fmaf(y.y, f, o.y);
+                for (int i = 0; i < 4; ++i) {
+                    const int w = min(w0 + w1 + i, NW - 1);
+                    y[i] = *reinterpret_cast<const float2 *>(reinterpret_cast<const float *>(smem + G::kRing) + w * G::kPart + col * RP + el);
+                    f[i] = s_ml[w][0][col].x;
                 }
-            const float top = s_all[col].x, sum = s_all[col].y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (w1 + i < n) o.x = fmaf(y[i].x, f[i], o.x), o.y = fmaf(y[i].y, f[i], o.y);
+            }
+            const float2 all = s_chain[c * Q8 + col];
             if (here) {
-                const float inv = top == -INFINITY ? 0.f : 1.f / sum;
+                const float inv = all.x == -INFINITY ? 0.f : 1.f / all.y;
                 *reinterpret_cast<uint32_t *>(a.out + (head0 + col) * D + el) = pack_bf16(o.x * inv, o.y * inv);
-                if (a.lse && el == 0) a.lse[head0 + col] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+                if (a.lse && el == 0) a.lse[head0 + col] = all.x == -INFINITY ? -INFINITY : (all.x + log2f(all.y)) * 0.6931471805599453f;
             } else {
                 __stcg(reinterpret_cast<float2 *>(a.ws_o + (slot * kMaxGroup + col) * D + el), o);
-                if (el == 0) __stcg(a.ws_ml + slot * kMaxGroup + col, make_float2(top, sum));
+                if (el == 0) __stcg(a.ws_ml + slot * kMaxGroup + col, all);
             }
         }
-        __syncthreads();
-        if (here) continue;
-        // The pair's parts lie with the blocks b0 .. b1: tile x is with worker ((x + 1) workers - 1) / all.  The last of them to arrive
-        // joins them, in their order.
-        const int workers = min((int)gridDim.x * NW, all);
-        const int b0 = (int)((((int64_t)pt.begin + 1) * workers - 1) / all) / NW, b1 = (int)(((int64_t)end * workers - 1) / all) / NW, n_parts = b1 - b0 + 1;
-        if (tid == 0) {
-            uint32_t before;                               // (back to 0 with the last)
-            asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(before) : "l"(a.ws_count + b0), "r"((uint32_t)(n_parts - 1)) : "memory");
-            s_last = before == (uint32_t)(n_parts - 1);
-        }
-        __syncthreads();
-        if (s_last)
-            for (int i = tid; i < a.g * (D / 2); i += NT) {
-                const int col = i / (D / 2), el = i % (D / 2) * 2;
-                float top = -INFINITY, sum = 0.f;
-                float2 o = make_float2(0.f, 0.f);
-                constexpr int kBatch = 10;                      // loads in flight
-                for (int p0 = 0; p0 < n_parts; p0 += kBatch) {
-                    float2 ml[kBatch];
-                    float2 y[kBatch];
-#pragma unroll
-                    for (int p = 0; p < kBatch; ++p) {
-                        const int i0 = min(p0 + p, n_parts - 1);
-                        const size_t from = 2 * (size_t)(b0 + i0) + (i0 == 0 ? 1 : 0);
-                        ml[p] = __ldcg(a.ws_ml + from * kMaxGroup + col);
-                        y[p] = __ldcg(reinterpret_cast<const float2 *>(a.ws_o + (from * kMaxGroup + col) * D + el));
-                        if (p0 + p >= n_parts) ml[p] = make_float2(-INFINITY, 0.f);
-                    }
-                    float mx = top;
-#pragma unroll
-                    for (int p = 0; p < kBatch; ++p) mx = fmaxf(mx, ml[p].x);
-                    const float ref = mx == -INFINITY ? 0.f : mx, f0 = ex2(top - ref);
-                    sum *= f0;
-                    o.x *= f0, o.y *= f0;
-#pragma unroll
-                    for (int p = 0; p < kBatch; ++p) {
-                        if (p0 + p >= n_parts) continue;
-                        const float f = ex2(ml[p].x - ref);
-                        sum = fmaf(ml[p].y, f, sum);
-                        o.x = fmaf(y[p].x, f, o.x), o.y = fmaf(y[p].y, f, o.y);
-                    }
-                    top = mx;
-                }
-                const float inv = top == -INFINITY ? 0.f : 1.f / sum;
-                *reinterpret_cast<uint32_t *>(a.out + (head0 + col) * D + el) = pack_bf16(o.x * inv, o.y * inv);
-                if (a.lse && el == 0) a.lse[head0 + col] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
-            }
     }
-
-    // requests without a key
-    for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
-        if (visible(a.seq_len[r], a).n == 0) {
-            for (int i = tid; i < a.H_q * D / 8; i += NT) stg(reinterpret_cast<uint4 *>(a.out + (size_t)r * a.H_q * D) + i, make_uint4(0, 0, 0, 0));
-            if (a.lse)
-                for (int i = tid; i < a.H_q; i += NT) a.lse[(size_t)r * a.H_q + i] = -INFINITY;
+    // A pair that leaves the block (two at most: one that began before it, one that goes on behind it) has parts with the blocks b0 .. b1;
+    // the last of them to arrive joins them, in their order.
+    if (s_leaves[0] < 0 && s_leaves[1] < 0) return empty_requests<D, NT, T>(a);
+    __syncthreads();
+    if (tid < 64 && lane == 0 && s_leaves[warp] >= 0) {
+        const int c = s_leaves[warp];
+        const Pair pt = s_part[max(c - 1, 0)][c == 0 ? 0 : 1];
+        const int b0 = worker_of(pt.begin, mine.workers, mine.all) / NW, b1 = worker_of(pt.begin + pt.tiles - 1, mine.workers, mine.all) / NW;
+        uint32_t before;                               // (back to 0 with the last)
+        asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(before) : "l"(a.ws_count + b0), "r"((uint32_t)(b1 - b0)) : "memory");
+        s_join[warp][0] = b0;
+        s_join[warp][1] = before == (uint32_t)(b1 - b0) ? b1 - b0 + 1 : 0;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        const int c = s_leaves[which];
+        if (c < 0) continue;
+        const int b0 = s_join[which][0], n_parts = s_join[which][1], pair = s_part[max(c - 1, 0)][c == 0 ? 0 : 1].pair;
+        if (n_parts == 0) continue;
+        const size_t head0 = (size_t)(pair / a.H_kv) * a.H_q + pair % a.H_kv * a.g;
+        for (int i = tid; i < a.g * (D / 2); i += NT) {
+            const int col = i / (D / 2), el = i % (D / 2) * 2;
+            float top = -INFINITY, sum = 0.f;
+            float2 o = make_float2(0.f, 0.f);
+            constexpr int kInFlight = 20;
+            for (int p0 = 0; p0 < n_parts; p0 += kInFlight) {
+                float2 ml[kInFlight], y[kInFlight];
+#pragma unroll
+                for (int p = 0; p < kInFlight; ++p)
+                    if (p0 + p < n_parts) {
+                        const size_t from = (2 * (size_t)(b0 + p0 + p) + (p0 + p == 0 ? 1 : 0)) * kMaxGroup + col;
+                        ml[p] = __ldcg(a.ws_ml + from);
+                        y[p] = __ldcg(reinterpret_cast<const float2 *>(a.ws_o + from * D + el));
+                    } else {
+                        ml[p] = make_float2(-INFINITY, 0.f);
+                        y[p] = make_float2(0.f, 0.f);
+                    }
+                float mx = top;
+#pragma unroll
+                for (int p = 0; p < kInFlight; ++p) mx = fmaxf(mx, ml[p].x);
+                const float ref = mx == -INFINITY ? 0.f : mx, f0 = ex2(top - ref);
+                sum *= f0;
+                o.x *= f0, o.y *= f0;
+#pragma unroll
+                for (int p = 0; p < kInFlight; ++p) {
+                    const float f = ex2(ml[p].x - ref);
+                    sum = fmaf(ml[p].y, f, sum);
+                    o.x = fmaf(y[p].x, f, o.x), o.y = fmaf(y[p].y, f, o.y);
+                }
+                top = mx;
+            }
+            const float inv = top == -INFINITY ? 0.f : 1.f / sum;
+            *reinterpret_cast<uint32_t *>(a.out + (head0 + col) * D + el) = pack_bf16(o.x * inv, o.y * inv);
+            if (a.lse && el == 0) a.lse[head0 + col] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
         }
+    }
+    empty_requests<D, NT, T>(a);
 }
 
 // Multiprocessors of the current device, 0 on failure.
@@ -822,7 +852,7 @@ bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) !=
 template <int D, bool F4, int NQ>
 cudaError_t launch_decode(const Args &a, int sms, cudaStream_t st) {
     using G = Geo<D, F4, NQ>;
-    auto kernel = a.page_size == 8 ? decode_attn_kernel<D, F4, NQ, true> : decode_attn_kernel<D, F4, NQ, false>;
+    auto kernel = a.page_size < G::kTile ? decode_attn_kernel<D, F4, NQ, true> : decode_attn_kernel<D, F4, NQ, false>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kBytes);
     if (e != cudaSuccess) {
         cudaGetLastError();
