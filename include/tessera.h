@@ -257,8 +257,8 @@ TESSERA_API int32_t tessera_kv_retain_fp8(const tessera_plan *plan, const void *
  * tokens, D/2 bytes each (byte i: element i in the low four bits, element i + D/2 in the high four), then four bf16 numbers for
  * every token: scale and least value of the head's first half, then of its second.  A half x_0 .. x_{D/2-1} of a 16-bit row
  * is kept as
- *     least = min x,   scale = bf16_rne(fp32((max x - min x) / 15)),   c_i = min(15, nearest integer to (x_i - least) / scale)
- * (ties to even; scale and codes 0 where the scale would be below 2^-126; a half that holds a NaN or an infinity, or whose range
+ *     least = min x,   scale = bf16_rne(fp32((max x - min x) / 15)),   c_i = nearest integer to fp32(x_i - least) / scale
+ * (ties to even, the quotient rounded to fp32; scale and codes 0 where the scale would be below 2^-100; a half that holds a NaN or an infinity, or whose range
  * is above fp32's, gets scale = least = NaN), and a code stands for fp32(scale c + least), one rounding.
  *   tessera_kv_retain_kv4        16-bit source pools -> 4-bit pools of num_pool_pages pages (the plan's destination).  With
  *                                TESSERA_FUSE_ROPE keys are rotated by the plan's shifts and rounded to bf16 first.

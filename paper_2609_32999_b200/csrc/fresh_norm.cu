@@ -193,17 +193,11 @@ decode_write_kernel(Fresh f, void *k_pool, void *v_pool, const __grid_constant__
         const size_t co = codes4_at<D>(page, off, h, s.page_size, s.H_kv), po = params4_at<D>(page, off, h, s.page_size, s.H_kv);
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            unpack_bf16x8(which ? vlo : lo, a);
-            unpack_bf16x8(which ? vhi : hi, b);
-            float s0, m0, s1, m1;
-            uint32_t c0[8], c1[8];
-            range4<D>(a, s0, m0);
-            range4<D>(b, s1, m1);
-            codes4(a, s0, m0, c0);
-            codes4(b, s1, m1, c1);
+            uint2 codes, numbers;
+            quantise4<D>(which ? vlo : lo, which ? vhi : hi, codes, numbers);
             uint8_t *pool = static_cast<uint8_t *>(which ? v_pool : k_pool);
-            *reinterpret_cast<uint2 *>(pool + co + c * 8) = pack4(c0, c1);
-            if (c == 0) *reinterpret_cast<uint2 *>(pool + po) = pack_params4(s0, m0, s1, m1);
+            *reinterpret_cast<uint2 *>(pool + co + c * 8) = codes;
+            if (c == 0) *reinterpret_cast<uint2 *>(pool + po) = numbers;
         }
     }
 }

@@ -46,9 +46,15 @@ kv4_kernel(const uint8_t *__restrict__ k_src, const uint8_t *__restrict__ v_src,
     grid_release();
     __syncthreads();
 
+    // Tasks go over the item's tokens first: four heads' worth of neighbouring threads are four tokens of one head, whose codes (256
+    // bytes) and numbers (32) lie side by side.
     const int page_shift = __ffs(page_size) - 1;
-    const int tasks_per_row = H_kv * CPH, n_tasks = it.count * tasks_per_row;
-    const int c = tid % CPH;             // kThreads and tasks_per_row are multiples of CPH: a head's threads stay together
+    const int tasks_per_head = it.count * CPH, n_tasks = H_kv * tasks_per_head;
+    const int c = tid % CPH;             // kThreads and tasks_per_head are multiples of CPH: a head's threads stay together
+    float2 cr[8];
+    if (ROTATE && it.row_step == 0)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) cr[i] = s_rope[cs_entry<D, INTERLEAVED>(c, i)];
     constexpr int U = TO_4BIT ? 1 : 2;   // tasks in flight per thread
     for (int t0 = tid; t0 < n_tasks; t0 += U * kThreads) {
         uint4 w[U][4];                   // 16-bit: K and V, both chunks; 4-bit: x, y of [0] K's codes and numbers, of [1] V's
@@ -59,8 +65,8 @@ kv4_kernel(const uint8_t *__restrict__ k_src, const uint8_t *__restrict__ v_src,
             const int t = t0 + u * kThreads;
             ok[u] = t < n_tasks;
             if (!ok[u]) continue;
-            tok[u] = t / tasks_per_row;
-            head[u] = (t - tok[u] * tasks_per_row) / CPH;
+            head[u] = t / tasks_per_head;
+            tok[u] = (t - head[u] * tasks_per_head) / CPH;
             const int src = s_src[tok[u]];
             if constexpr (TO_4BIT) {
                 const size_t o = ((size_t)src * H_kv + head[u]) * (D / 8) + c;
@@ -83,9 +89,8 @@ kv4_kernel(const uint8_t *__restrict__ k_src, const uint8_t *__restrict__ v_src,
         for (int u = 0; u < U; ++u) {
             if (!ok[u]) continue;
             const int dst = s_dst[tok[u]];
-            float2 cr[8];
-            if (ROTATE) {
-                const int sr = it.row_step == 0 ? 0 : (it.row_step < 0 ? it.count - 1 - tok[u] : tok[u]);
+            if (ROTATE && it.row_step != 0) {
+                const int sr = it.row_step < 0 ? it.count - 1 - tok[u] : tok[u];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) cr[i] = s_rope[sr * (D / 2) + cs_entry<D, INTERLEAVED>(c, i)];
             }
@@ -94,24 +99,20 @@ kv4_kernel(const uint8_t *__restrict__ k_src, const uint8_t *__restrict__ v_src,
                 const int off = dst & (page_size - 1);
                 const size_t co = codes4_at<D>(dst >> page_shift, off, head[u], page_size, H_kv) + c * 8;
                 const size_t po = params4_at<D>(dst >> page_shift, off, head[u], page_size, H_kv);
+                if (ROTATE) {
+                    unpack_bf16x8(w[u][0], lo);
+                    unpack_bf16x8(w[u][1], hi);
+                    rotate_f<INTERLEAVED>(lo, hi, cr);
+                    w[u][0] = pack_bf16x8(lo);                    // what a 16-bit row would hold
+                    w[u][1] = pack_bf16x8(hi);
+                }
 #pragma unroll
                 for (int which = 0; which < 2; ++which) {
-                    unpack_bf16x8(w[u][2 * which], lo);
-                    unpack_bf16x8(w[u][2 * which + 1], hi);
-                    if (ROTATE && which == 0) {
-                        rotate_f<INTERLEAVED>(lo, hi, cr);
-                        unpack_bf16x8(pack_bf16x8(lo), lo);       // what a 16-bit row would hold
-                        unpack_bf16x8(pack_bf16x8(hi), hi);
-                    }
-                    float s0, m0, s1, m1;
-                    uint32_t c0[8], c1[8];
-                    range4<D>(lo, s0, m0);
-                    range4<D>(hi, s1, m1);
-                    codes4(lo, s0, m0, c0);
-                    codes4(hi, s1, m1, c1);
+                    uint2 codes, numbers;
+                    quantise4<D>(w[u][2 * which], w[u][2 * which + 1], codes, numbers);
                     uint8_t *pool = which ? v_dst : k_dst;
-                    *reinterpret_cast<uint2 *>(pool + co) = pack4(c0, c1);
-                    if (c == 0) *reinterpret_cast<uint2 *>(pool + po) = pack_params4(s0, m0, s1, m1);
+                    *reinterpret_cast<uint2 *>(pool + co) = codes;
+                    if (c == 0) *reinterpret_cast<uint2 *>(pool + po) = numbers;
                 }
             } else {
                 const size_t o = ((size_t)dst * H_kv + head[u]) * (D / 8) + c;

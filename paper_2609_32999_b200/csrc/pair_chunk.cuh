@@ -65,77 +65,86 @@ struct HeadLanes {
         for (int o = kN / 2; o > 0; o /= 2) v += __shfl_xor_sync(mask(), v, o);
         return v;
     }
-    // (the largest of both arguments over the head's threads; NaN is lost, see quantise4)
-    __device__ static float max(float v) {
-#pragma unroll
-        for (int o = kN / 2; o > 0; o /= 2) v = fmaxf(v, __shfl_xor_sync(mask(), v, o));
-        return v;
-    }
 };
 
 // ---- 4-bit rows.  A half of a head (D/2 elements) is kept as the least value m (a bf16 number, as the elements are), a
-// scale s = bf16_rne((M - m) / 15) with M the greatest, and codes c = the nearest integer to (x - m) / s, ties to even, at
-// most 15; it stands for s c + m.  s is 0, and so are the codes, where it would be below 2^-126.  A half that holds a NaN or an
-// infinity, or whose range is above fp32's, is kept as s = m = NaN.
+// scale s = bf16_rne((M - m) / 15) with M the greatest, and codes c = the nearest integer to (x - m) / s, ties to even; it stands
+// for s c + m.  (s is within 2^-8 of (M - m) / 15, so no quotient reaches 15.5.)  s is 0, and so are the codes, where it would be
+// below 2^-100 (so that no rest of a quotient is subnormal).  A half that holds a NaN or an infinity, or whose range is above fp32's, is kept as s = m = NaN.
 
-// Scale and least value of a half whose elements the head's threads hold, 8 each.
+// Scales and least values of both halves of a head, whose elements the head's threads hold, 8 of each half as they were loaded.
+// (Comparisons in pairs of bf16: the extremes are elements.)
 template <int D>
-__device__ __forceinline__ void range4(const float (&x)[8], float &scale, float &least) {
-    float lo = x[0], hi = x[0], bad = 0.f;
+__device__ __forceinline__ void ranges4(const uint4 &lo, const uint4 &hi, float (&scale)[2], float (&least)[2]) {
+    auto pairs = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162 *>(&x); };
+    auto bits = [](__nv_bfloat162 x) { return *reinterpret_cast<const uint32_t *>(&x); };
+    const __nv_bfloat162 top0 = __hmax2_nan(__hmax2_nan(pairs(lo.x), pairs(lo.y)), __hmax2_nan(pairs(lo.z), pairs(lo.w)));
+    const __nv_bfloat162 top1 = __hmax2_nan(__hmax2_nan(pairs(hi.x), pairs(hi.y)), __hmax2_nan(pairs(hi.z), pairs(hi.w)));
+    const __nv_bfloat162 low0 = __hmin2_nan(__hmin2_nan(pairs(lo.x), pairs(lo.y)), __hmin2_nan(pairs(lo.z), pairs(lo.w)));
+    const __nv_bfloat162 low1 = __hmin2_nan(__hmin2_nan(pairs(hi.x), pairs(hi.y)), __hmin2_nan(pairs(hi.z), pairs(hi.w)));
+    // (first half, second half) from here on
+    uint32_t top = bits(__hmax2_nan(pairs(__byte_perm(bits(top0), bits(top1), 0x5410)), pairs(__byte_perm(bits(top0), bits(top1), 0x7632))));
+    uint32_t low = bits(__hmin2_nan(pairs(__byte_perm(bits(low0), bits(low1), 0x5410)), pairs(__byte_perm(bits(low0), bits(low1), 0x7632))));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-        bad = fmaf(x[i], 0.f, bad);            // NaN where an element is NaN or infinite, 0 otherwise
+    for (int o = HeadLanes<D>::kN / 2; o > 0; o /= 2) {
+        top = bits(__hmax2_nan(pairs(top), pairs(__shfl_xor_sync(HeadLanes<D>::mask(), top, o))));
+        low = bits(__hmin2_nan(pairs(low), pairs(__shfl_xor_sync(HeadLanes<D>::mask(), low, o))));
     }
-    hi = HeadLanes<D>::max(hi);
-    lo = -HeadLanes<D>::max(-lo);
-    const float range = __fsub_rn(hi, lo) + HeadLanes<D>::sum(bad);
-    const bool fine = range <= 3.402823466e38f;
-    const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(range, 15.f)));
-    least = fine ? lo : __int_as_float(0x7fc00000);
-    scale = fine ? (s < 1.17549435e-38f ? 0.f : s) : least;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float m = __uint_as_float(h ? low & 0xffff0000u : low << 16);
+        const float range = __fsub_rn(__uint_as_float(h ? top & 0xffff0000u : top << 16), m);
+        const bool fine = range <= 3.402823466e38f;             // (of infinities: NaN or infinite)
+        const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(range, 15.f)));
+        least[h] = fine ? m : __int_as_float(0x7fc00000);
+        scale[h] = fine ? (s < 7.8886091e-31f ? 0.f : s) : least[h];
+    }
 }
-// Codes of 8 elements, 0 where there is no scale.  The quotient's integer is corrected where its rounding could have moved it
-// across a border: c s is exact, so x - m - c s tells on which side of half a step the element lies.
+// Codes of 8 elements as the low bytes of eight numbers.  With inv the rounded reciprocal, q = d inv corrected by the exact
+// rest d - q s is the rounded quotient, exact where it lies half way between integers, and adding 1.5 2^23 rounds that
+// to an integer, ties to even.  (Of a scale of 0 or NaN: anything.)
 __device__ __forceinline__ void codes4(const float (&x)[8], float scale, float least, uint32_t (&c)[8]) {
-    const bool some = scale > 0.f;
-    const float inv = some ? __frcp_rn(scale) : 0.f, half = 0.5f * scale;
+    const float inv = __frcp_rn(scale);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float d = __fsub_rn(x[i], least);
-        float n = rintf(d * inv);
-        const float rest = fmaf(-n, scale, d);
-        const bool odd = (__float2int_rn(n) & 1) != 0;
-        if (rest > half || (rest == half && odd)) n += 1.f;
-        if (rest < -half || (rest == -half && odd)) n -= 1.f;
-        c[i] = some ? (uint32_t)fminf(fmaxf(n, 0.f), 15.f) : 0u;
+        const float q = __fmul_rn(d, inv), rest = fmaf(-q, scale, d);
+        c[i] = __float_as_uint(__fadd_rn(fmaf(rest, inv, q), 12582912.f));
     }
 }
-// 8 bytes of a row of codes: low four bits the elements of the first half, high four those D/2 later.
-__device__ __forceinline__ uint2 pack4(const uint32_t (&lo)[8], const uint32_t (&hi)[8]) {
-    uint32_t w[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        w[k] = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[k] |= (lo[4 * k + i] | hi[4 * k + i] << 4) << (8 * i);
-    }
-    return make_uint2(w[0], w[1]);
+// 8 bytes of a row of codes: low four bits the elements of the first half, high four those D/2 later.  some: which halves have codes.
+__device__ __forceinline__ uint2 pack4(const uint32_t (&lo)[8], const uint32_t (&hi)[8], bool some_lo, bool some_hi) {
+    const uint32_t on_lo = some_lo ? 0x0f0f0f0fu : 0u, on_hi = some_hi ? 0x0f0f0f0fu : 0u;
+    auto bytes = [](const uint32_t *c) { return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410); };
+    return make_uint2((bytes(hi) & on_hi) * 16u + (bytes(lo) & on_lo), (bytes(hi + 4) & on_hi) * 16u + (bytes(lo + 4) & on_lo));
 }
 // Scale and least value of both halves as the pool holds them: (s0, m0, s1, m1), bf16.
 __device__ __forceinline__ uint2 pack_params4(float s0, float m0, float s1, float m1) {
     const __nv_bfloat162 a = __floats2bfloat162_rn(s0, m0), b = __floats2bfloat162_rn(s1, m1);
     return make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
 }
+// A thread's 8 bytes of codes of a head's chunk pair, and the head's numbers.
+template <int D>
+__device__ __forceinline__ void quantise4(const uint4 &lo, const uint4 &hi, uint2 &codes, uint2 &numbers) {
+    float s[2], m[2], f[8];
+    uint32_t c0[8], c1[8];
+    ranges4<D>(lo, hi, s, m);
+    unpack_bf16x8(lo, f);
+    codes4(f, s[0], m[0], c0);
+    unpack_bf16x8(hi, f);
+    codes4(f, s[1], m[1], c1);
+    codes = pack4(c0, c1, s[0] > 0.f, s[1] > 0.f);
+    numbers = pack_params4(s[0], m[0], s[1], m[1]);
+}
+// A code becomes a number as the last byte of 2^23's mantissa.
 __device__ __forceinline__ void unpack4(const uint2 &w, const uint2 &p, float (&lo)[8], float (&hi)[8]) {
     const float s0 = __uint_as_float(p.x << 16), m0 = __uint_as_float(p.x & 0xffff0000u);
     const float s1 = __uint_as_float(p.y << 16), m1 = __uint_as_float(p.y & 0xffff0000u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint32_t b = ((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 0xffu;
-        lo[i] = fmaf((float)(b & 15u), s0, m0);
-        hi[i] = fmaf((float)(b >> 4), s1, m1);
+        const uint32_t b = i < 4 ? w.x : w.y;
+        lo[i] = fmaf(__uint_as_float(__byte_perm(b & 0x0f0f0f0fu, 0x4b000000u, 0x7650 + (i & 3))) - 8388608.f, s0, m0);
+        hi[i] = fmaf(__uint_as_float(__byte_perm((b >> 4) & 0x0f0f0f0fu, 0x4b000000u, 0x7650 + (i & 3))) - 8388608.f, s1, m1);
     }
 }
 // Where a token's row lies in a 4-bit pool [pages][H_kv][page_size * (D/2 + 8)]: its codes and its four numbers.

@@ -9,9 +9,9 @@ def quantise(x):
     span = top - least
     good = torch.isfinite(y).all(-1) & torch.isfinite(span)
     scale = (span / torch.full_like(span, 15.0)).to(torch.bfloat16).float()
-    scale = torch.where(scale < 2.0 ** -126, 0.0, scale)
+    scale = torch.where(scale < 2.0 ** -100, 0.0, scale)
     least, scale = torch.where(good, least, torch.nan), torch.where(good, scale, torch.nan)
-    quotient = (y.double() - least.double()[..., None]) / torch.where(scale > 0, scale, 1.0).double()[..., None]
+    quotient = (y - least[..., None]) / torch.where(scale > 0, scale, 1.0)[..., None]
     codes = torch.where((scale > 0)[..., None], quotient.round(), 0.0).nan_to_num(0.0).clamp(0, 15).int()
     return scale, least, codes
 

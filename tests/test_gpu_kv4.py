@@ -66,11 +66,12 @@ def strange(x):
     x[6, :, 0] = float("-inf")
     x[7, :, 1], x[7, :, 2] = 3e38, -3e38                                # range above fp32's
     x[8] = torch.randn(h, d, device=x.device).to(x.dtype) * 2e38 / 4
-    x[9] = torch.randn(h, d, device=x.device).to(x.dtype) * 1e-38       # ranges around the smallest normal number
+    x[9] = torch.randn(h, d, device=x.device).to(x.dtype) * 3e-30       # scales around the smallest that is kept
     x[10] = torch.randn(h, d, device=x.device).to(x.dtype) * 1e-40
     x[11] = 1000 + torch.randn(h, d, device=x.device).to(x.dtype)
     x[12, :, : d // 2] = 1e30
     x[13] = -x[2]
+    x[14] = (torch.arange(d, device=x.device) % 16) * 2.0 ** -96
 
 
 @pytest.mark.parametrize("hq,h,d,page,pairing", SHAPES)
