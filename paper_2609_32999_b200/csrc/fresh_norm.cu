@@ -54,9 +54,9 @@ __device__ __forceinline__ void norm_chunks(float (&lo)[8], float (&hi)[8], cons
 
 // A block owns kRowsPerBlock recompute rows, kThreadsPerRow threads each.  A thread keeps one chunk index c, so the eight
 // (cos, sin) of its pairs stay in registers for all heads of its row, and it has kFlight heads' loads in flight.
-constexpr int kRowsPerBlock = 4, kThreadsPerRow = 64, kFlight = 4;
+constexpr int kRowsPerBlock = 4, kThreadsPerRow = 64, kFlight = 2;
 template <int D, bool INTERLEAVED>
-__global__ void __launch_bounds__(kRowsPerBlock *kThreadsPerRow)
+__global__ void __launch_bounds__(kRowsPerBlock *kThreadsPerRow, 4)
 extend_norm_kernel(Fresh f, uint4 *k_pool, uint4 *v_pool, uint4 *k_cache, uint4 *v_cache, const int32_t *__restrict__ q_pos,
                    const int32_t *__restrict__ fresh_dst, const int32_t *__restrict__ retain_dst, const double *__restrict__ inv_freq,
                    int n_q, int H_q, int H_kv) {

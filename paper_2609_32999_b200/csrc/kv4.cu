@@ -25,7 +25,7 @@ constexpr int kThreads = 256;
 
 // One thread block per GatherItem.
 template <int D, bool TO_4BIT, bool ROTATE, bool INTERLEAVED>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 kv4_kernel(const uint8_t *__restrict__ k_src, const uint8_t *__restrict__ v_src, uint8_t *__restrict__ k_dst, uint8_t *__restrict__ v_dst,
            const int32_t *__restrict__ g_src, const int32_t *__restrict__ g_dst, const GatherItem *__restrict__ items,
            const float2 *__restrict__ rope, int H_kv, int page_size) {
@@ -46,85 +46,75 @@ kv4_kernel(const uint8_t *__restrict__ k_src, const uint8_t *__restrict__ v_src,
     grid_release();
     __syncthreads();
 
-    // Tasks go over the item's tokens first: four heads' worth of neighbouring threads are four tokens of one head, whose codes (256
-    // bytes) and numbers (32) lie side by side.
-    const int page_shift = __ffs(page_size) - 1;
-    const int tasks_per_head = it.count * CPH, n_tasks = H_kv * tasks_per_head;
-    const int c = tid % CPH;             // kThreads and tasks_per_head are multiples of CPH: a head's threads stay together
+    // A thread keeps its token and its chunk pair and goes through the heads: slots, places and (cos, sin) are worked out once, and four
+    // groups of neighbouring threads are four tokens of one head, whose codes (256 bytes) and numbers (32) lie side by side.
+    // Items of fewer tokens have several heads under way at once.
+    const int slots = it.count > 16 ? 32 : it.count > 8 ? 16 : 8;
+    const int c = tid % CPH, tok = tid / CPH % slots, page_shift = __ffs(page_size) - 1;
+    if (tok >= it.count) return;         // (the threads of a head together)
     float2 cr[8];
-    if (ROTATE && it.row_step == 0)
+    if (ROTATE) {
+        const float2 *row = s_rope + (it.row_step == 0 ? 0 : it.row_step < 0 ? it.count - 1 - tok : tok) * (D / 2);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) cr[i] = s_rope[cs_entry<D, INTERLEAVED>(c, i)];
-    constexpr int U = TO_4BIT ? 1 : 2;   // tasks in flight per thread
-    for (int t0 = tid; t0 < n_tasks; t0 += U * kThreads) {
-        uint4 w[U][4];                   // 16-bit: K and V, both chunks; 4-bit: x, y of [0] K's codes and numbers, of [1] V's
-        int tok[U], head[U];
-        bool ok[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int t = t0 + u * kThreads;
-            ok[u] = t < n_tasks;
-            if (!ok[u]) continue;
-            head[u] = t / tasks_per_head;
-            tok[u] = (t - head[u] * tasks_per_head) / CPH;
-            const int src = s_src[tok[u]];
-            if constexpr (TO_4BIT) {
-                const size_t o = ((size_t)src * H_kv + head[u]) * (D / 8) + c;
-                const uint4 *k = reinterpret_cast<const uint4 *>(k_src) + o, *v = reinterpret_cast<const uint4 *>(v_src) + o;
-                w[u][0] = ldg_stream(k);
-                w[u][1] = ldg_stream(k + HALF);
-                w[u][2] = ldg_stream(v);
-                w[u][3] = ldg_stream(v + HALF);
-            } else {
-                const int off = src & (page_size - 1);
-                const size_t co = codes4_at<D>(src >> page_shift, off, head[u], page_size, H_kv) + c * 8;
-                const size_t po = params4_at<D>(src >> page_shift, off, head[u], page_size, H_kv);
-                const uint2 kc = ldg_pieces(reinterpret_cast<const uint2 *>(k_src + co)), kp = ldg_pieces(reinterpret_cast<const uint2 *>(k_src + po));
-                const uint2 vc = ldg_pieces(reinterpret_cast<const uint2 *>(v_src + co)), vp = ldg_pieces(reinterpret_cast<const uint2 *>(v_src + po));
-                w[u][0] = make_uint4(kc.x, kc.y, kp.x, kp.y);
-                w[u][1] = make_uint4(vc.x, vc.y, vp.x, vp.y);
+        for (int i = 0; i < 8; ++i) cr[i] = row[cs_entry<D, INTERLEAVED>(c, i)];
+    }
+    const int src = s_src[tok], dst = s_dst[tok], wide = TO_4BIT ? src : dst, narrow = TO_4BIT ? dst : src;
+    const int h0 = tid / CPH / slots, step = kThreads / CPH / slots;
+    const size_t head4 = (size_t)page_size * (D / 2 + 8);
+    const size_t o16 = ((size_t)wide * H_kv + h0) * (D / 8) + c;
+    const size_t oc = codes4_at<D>(narrow >> page_shift, narrow & (page_size - 1), h0, page_size, H_kv) + c * 8;
+    const size_t on = params4_at<D>(narrow >> page_shift, narrow & (page_size - 1), h0, page_size, H_kv);
+    if constexpr (TO_4BIT) {
+        const uint4 *k = reinterpret_cast<const uint4 *>(k_src) + o16, *v = reinterpret_cast<const uint4 *>(v_src) + o16;
+        uint8_t *kd = k_dst + oc, *vd = v_dst + oc, *kn = k_dst + on, *vn = v_dst + on;
+        for (int h = h0; h < H_kv; h += step, k += step * (D / 8), v += step * (D / 8)) {
+            uint4 klo = ldg_stream(k), khi = ldg_stream(k + HALF);
+            const uint4 vlo = ldg_stream(v), vhi = ldg_stream(v + HALF);
+            if (ROTATE) {
+                float lo[8], hi[8];
+                unpack_bf16x8(klo, lo);
+                unpack_bf16x8(khi, hi);
+                rotate_f<INTERLEAVED>(lo, hi, cr);
+                klo = pack_bf16x8(lo);                    // what a 16-bit row would hold
+                khi = pack_bf16x8(hi);
             }
+            uint2 codes, numbers;
+            quantise4<D>(klo, khi, codes, numbers);
+            *reinterpret_cast<uint2 *>(kd) = codes;
+            if (c == 0) *reinterpret_cast<uint2 *>(kn) = numbers;
+            quantise4<D>(vlo, vhi, codes, numbers);
+            *reinterpret_cast<uint2 *>(vd) = codes;
+            if (c == 0) *reinterpret_cast<uint2 *>(vn) = numbers;
+            kd += step * head4, vd += step * head4, kn += step * head4, vn += step * head4;
         }
+    } else {
+        const uint8_t *kc = k_src + oc, *vc = v_src + oc, *kn = k_src + on, *vn = v_src + on;
+        uint4 *kd = reinterpret_cast<uint4 *>(k_dst) + o16, *vd = reinterpret_cast<uint4 *>(v_dst) + o16;
+        constexpr int U = 2;             // heads in flight
+        for (int h = h0; h < H_kv; h += U * step) {
+            uint2 w[U][4];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (!ok[u]) continue;
-            const int dst = s_dst[tok[u]];
-            if (ROTATE && it.row_step != 0) {
-                const int sr = it.row_step < 0 ? it.count - 1 - tok[u] : tok[u];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) cr[i] = s_rope[sr * (D / 2) + cs_entry<D, INTERLEAVED>(c, i)];
-            }
-            float lo[8], hi[8];
-            if constexpr (TO_4BIT) {
-                const int off = dst & (page_size - 1);
-                const size_t co = codes4_at<D>(dst >> page_shift, off, head[u], page_size, H_kv) + c * 8;
-                const size_t po = params4_at<D>(dst >> page_shift, off, head[u], page_size, H_kv);
-                if (ROTATE) {
-                    unpack_bf16x8(w[u][0], lo);
-                    unpack_bf16x8(w[u][1], hi);
-                    rotate_f<INTERLEAVED>(lo, hi, cr);
-                    w[u][0] = pack_bf16x8(lo);                    // what a 16-bit row would hold
-                    w[u][1] = pack_bf16x8(hi);
+            for (int u = 0; u < U; ++u)
+                if (h + u * step < H_kv) {
+                    w[u][0] = ldg_pieces(reinterpret_cast<const uint2 *>(kc + u * step * head4));
+                    w[u][1] = ldg_pieces(reinterpret_cast<const uint2 *>(kn + u * step * head4));
+                    w[u][2] = ldg_pieces(reinterpret_cast<const uint2 *>(vc + u * step * head4));
+                    w[u][3] = ldg_pieces(reinterpret_cast<const uint2 *>(vn + u * step * head4));
                 }
 #pragma unroll
-                for (int which = 0; which < 2; ++which) {
-                    uint2 codes, numbers;
-                    quantise4<D>(w[u][2 * which], w[u][2 * which + 1], codes, numbers);
-                    uint8_t *pool = which ? v_dst : k_dst;
-                    *reinterpret_cast<uint2 *>(pool + co) = codes;
-                    if (c == 0) *reinterpret_cast<uint2 *>(pool + po) = numbers;
+            for (int u = 0; u < U; ++u)
+                if (h + u * step < H_kv) {
+                    float lo[8], hi[8];
+                    unpack4(w[u][0], w[u][1], lo, hi);
+                    if (ROTATE) rotate_f<INTERLEAVED>(lo, hi, cr);
+                    stg(kd, pack_bf16x8(lo));
+                    stg(kd + HALF, pack_bf16x8(hi));
+                    unpack4(w[u][2], w[u][3], lo, hi);
+                    stg(vd, pack_bf16x8(lo));
+                    stg(vd + HALF, pack_bf16x8(hi));
+                    kd += step * (D / 8), vd += step * (D / 8);
                 }
-            } else {
-                const size_t o = ((size_t)dst * H_kv + head[u]) * (D / 8) + c;
-#pragma unroll
-                for (int which = 0; which < 2; ++which) {
-                    unpack4(make_uint2(w[u][which].x, w[u][which].y), make_uint2(w[u][which].z, w[u][which].w), lo, hi);
-                    if (ROTATE && which == 0) rotate_f<INTERLEAVED>(lo, hi, cr);
-                    uint4 *pool = reinterpret_cast<uint4 *>(which ? v_dst : k_dst) + o;
-                    stg(pool, pack_bf16x8(lo));
-                    stg(pool + HALF, pack_bf16x8(hi));
-                }
-            }
+            kc += U * step * head4, vc += U * step * head4, kn += U * step * head4, vn += U * step * head4;
         }
     }
 }

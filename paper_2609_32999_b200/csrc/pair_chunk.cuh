@@ -72,6 +72,13 @@ struct HeadLanes {
 // for s c + m.  (s is within 2^-8 of (M - m) / 15, so no quotient reaches 15.5.)  s is 0, and so are the codes, where it would be
 // below 2^-100 (so that no rest of a quotient is subnormal).  A half that holds a NaN or an infinity, or whose range is above fp32's, is kept as s = m = NaN.
 
+// a / b from an approximate reciprocal of b by Markstein's correction (IBM J. Res. Dev. 34, 1990): the rest a - q b is exact, so
+// q + rest inv is the rounded quotient, and the quotient itself where that is a number (half way between integers, say).
+__device__ __forceinline__ float quotient(float a, float b, float inv) {
+    const float q = __fmul_rn(a, inv);
+    return fmaf(fmaf(-q, b, a), inv, q);
+}
+
 // Scales and least values of both halves of a head, whose elements the head's threads hold, 8 of each half as they were loaded.
 // (Comparisons in pairs of bf16: the extremes are elements.)
 template <int D>
@@ -95,21 +102,20 @@ __device__ __forceinline__ void ranges4(const uint4 &lo, const uint4 &hi, float 
         const float m = __uint_as_float(h ? low & 0xffff0000u : low << 16);
         const float range = __fsub_rn(__uint_as_float(h ? top & 0xffff0000u : top << 16), m);
         const bool fine = range <= 3.402823466e38f;             // (of infinities: NaN or infinite)
-        const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(range, 15.f)));
+        const float s = __bfloat162float(__float2bfloat16_rn(quotient(range, 15.f, 1.f / 15.f)));
         least[h] = fine ? m : __int_as_float(0x7fc00000);
         scale[h] = fine ? (s < 7.8886091e-31f ? 0.f : s) : least[h];
     }
 }
-// Codes of 8 elements as the low bytes of eight numbers.  With inv the rounded reciprocal, q = d inv corrected by the exact
-// rest d - q s is the rounded quotient, exact where it lies half way between integers, and adding 1.5 2^23 rounds that
-// to an integer, ties to even.  (Of a scale of 0 or NaN: anything.)
+// Codes of 8 elements as the low bytes of eight numbers: adding 1.5 2^23 rounds a quotient to an integer, ties to even.  (Of a
+// scale of 0 or NaN: anything.)
 __device__ __forceinline__ void codes4(const float (&x)[8], float scale, float least, uint32_t (&c)[8]) {
-    const float inv = __frcp_rn(scale);
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(scale));
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float d = __fsub_rn(x[i], least);
-        const float q = __fmul_rn(d, inv), rest = fmaf(-q, scale, d);
-        c[i] = __float_as_uint(__fadd_rn(fmaf(rest, inv, q), 12582912.f));
+        c[i] = __float_as_uint(__fadd_rn(quotient(d, scale, inv), 12582912.f));
     }
 }
 // 8 bytes of a row of codes: low four bits the elements of the first half, high four those D/2 later.  some: which halves have codes.
