@@ -161,30 +161,32 @@ def _model_cfg(sh, inv: Optional[np.ndarray]) -> ModelCfg:
                     int(sh.rope_pairing), float(sh.sm_scale))
 
 
-def _expect(what: str, t, device, dtypes, shape, rows: bool = False) -> None:
+def _expect(what: str, t, index: int, dtype, shape, rows: bool = False) -> None:
     """Device, type and shape of a tensor; contiguous, or (rows) with heads side by side inside rows any distance apart."""
-    if t.device != device or str(t.dtype) not in dtypes or tuple(t.shape) != shape:
-        raise ValueError("%s: expected %s of %s on %s, got %s of %s on %s"
-                         % (what, shape, " / ".join(dtypes), device, tuple(t.shape), t.dtype, t.device))
-    if not (t.is_contiguous() or (rows and t.stride()[1:] == (shape[2], 1) and t.stride(0) >= shape[1] * shape[2])):
+    if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+        return
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        raise ValueError("%s: expected %s of %s on device %d, got %s of %s on device %d"
+                         % (what, tuple(shape), dtype, index, tuple(t.shape), t.dtype, t.get_device()))
+    if not (rows and t.stride()[1:] == (shape[2], 1) and t.stride(0) >= shape[1] * shape[2]):
         raise ValueError("%s: strides %s" % (what, tuple(t.stride())))
 
 
-_BF16, _I32, _F32, _BYTES = ("torch.bfloat16",), ("torch.int32",), ("torch.float32",), ("torch.uint8",)
-
-
-def _fresh_rows(sh, n: int, device, q, q_out, k, v, q_weight, k_weight, eps) -> FreshRows:
+def _fresh_rows(sh, n: int, index: int, q, q_out, k, v, q_weight, k_weight, eps) -> FreshRows:
+    from torch import bfloat16
     hq, h, d = sh.num_q_heads, sh.num_kv_heads, sh.head_dim
     if q is not None:
-        _expect("q", q, device, _BF16, (n, hq, d), rows=True)
-        _expect("q_out", q_out, device, _BF16, (n, hq, d))
-    _expect("k_new", k, device, _BF16, (n, h, d), rows=True)
-    _expect("v_new", v, device, _BF16, (n, h, d), rows=True)
-    for what, t in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if t is not None:
-            _expect(what, t, device, _BF16, (d,))
-    row = [0 if n < 2 or t is None else t.stride(0) for t in (q, k, v)]
-    return FreshRows(_dev(q), _dev(k), _dev(v), None if q is None else _dev(q_out), *row, _dev(q_weight), _dev(k_weight), eps)
+        _expect("q", q, index, bfloat16, (n, hq, d), rows=True)
+        _expect("q_out", q_out, index, bfloat16, (n, hq, d))
+    _expect("k_new", k, index, bfloat16, (n, h, d), rows=True)
+    _expect("v_new", v, index, bfloat16, (n, h, d), rows=True)
+    if q_weight is not None:
+        _expect("q_weight", q_weight, index, bfloat16, (d,))
+    if k_weight is not None:
+        _expect("k_weight", k_weight, index, bfloat16, (d,))
+    one = n < 2                            # (the stride of a single row means nothing)
+    return FreshRows(_dev(q), k.data_ptr(), v.data_ptr(), None if q is None else q_out.data_ptr(), 0 if one or q is None else q.stride(0),
+                     0 if one else k.stride(0), 0 if one else v.stride(0), _dev(q_weight), _dev(k_weight), eps)
 
 
 class Plan:
@@ -289,7 +291,7 @@ class Plan:
                           v_cache=None, stream=None) -> None:
         """extend_write with per-head norms of q and k before the rotation, q written to q_out (q itself, or another tensor); q, k_new_raw and
         v_new may be slices [n_q, heads, D] of a fused projection.  q None: keys and values alone."""
-        rows = _fresh_rows(self.shape, int(self.info.n_q), k_new_raw.device, q, q_out, k_new_raw, v_new, q_weight, k_weight, eps)
+        rows = _fresh_rows(self.shape, int(self.info.n_q), k_new_raw.get_device(), q, q_out, k_new_raw, v_new, q_weight, k_weight, eps)
         _check(_lib.tessera_extend_write_norm(self._h, _dev(k_pool), _dev(v_pool), ctypes.byref(rows), _dev(k_cache), _dev(v_cache), _stream(stream)))
 
     def partial_prefill_attn(self, k_pool, v_pool, q, k_new, v_new, out, lse=None, stream=None) -> None:
@@ -352,65 +354,70 @@ class Decode:
 
     def __init__(self, shape, block_table, seq_lens, num_pool_pages: int, window: int = 0, n_sink: int = 0, inv_freq=None, workspace=None):
         import torch
-        self.shape, self.batch, self.device = shape, int(seq_lens.shape[0]), block_table.device
         if block_table.device.type != "cuda" or block_table.dim() != 2:
             raise ValueError("block_table: a [batch, max_pages] tensor on a CUDA device")
-        _expect("block_table", block_table, self.device, _I32, (self.batch, int(block_table.shape[1])))
-        _expect("seq_lens", seq_lens, self.device, _I32, (self.batch,))
-        self._index, self._current = self.device.index, torch._C._cuda_getDevice
+        self.shape, self.batch, self.device = shape, int(seq_lens.shape[0]), block_table.device
+        self._index = block_table.get_device()
+        self._current, self._raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        self._bf16, self._f32, self._u8 = torch.bfloat16, torch.float32, torch.uint8
+        _expect("block_table", block_table, self._index, torch.int32, (self.batch, int(block_table.shape[1])))
+        _expect("seq_lens", seq_lens, self._index, torch.int32, (self.batch,))
         # (the frequencies here, once: 64 powers in every call's host time otherwise)
         d = shape.head_dim
         self._inv = np.ascontiguousarray([float(shape.rope_theta) ** (-2.0 * m / d) for m in range(d // 2)] if inv_freq is None else inv_freq, dtype=np.float64)
         self._cfg = _model_cfg(shape, self._inv)
         self.block_table, self.seq_lens, self.num_pool_pages = block_table, seq_lens, int(num_pool_pages)
         self._desc = DecodeDesc(self.batch, int(block_table.shape[1]), _dev(block_table), _dev(seq_lens), self.num_pool_pages, int(window), int(n_sink))
+        self._args = ctypes.byref(self._cfg), ctypes.byref(self._desc)
         need = ctypes.c_int64(0)
         with torch.cuda.device(self.device):
-            _check(_lib.tessera_decode_workspace_bytes(ctypes.byref(self._cfg), ctypes.byref(need)))
+            _check(_lib.tessera_decode_workspace_bytes(self._args[0], ctypes.byref(need)))
         self.workspace = torch.zeros(need.value, dtype=torch.uint8, device=self.device) if workspace is None else workspace
-        _expect("workspace", self.workspace, self.device, _BYTES, (int(self.workspace.numel()),))
+        _expect("workspace", self.workspace, self._index, torch.uint8, (int(self.workspace.numel()),))
         self._pool = (self.num_pool_pages, shape.page_size, shape.num_kv_heads, d)
         self._pool4 = pool4_shape(shape, self.num_pool_pages)
-        self._q = (self.batch, shape.num_q_heads, d)
+        self._q, self._lse = (self.batch, shape.num_q_heads, d), (self.batch, shape.num_q_heads)
 
-    def _pools(self, k_pool, v_pool, dtypes, shape) -> None:
+    def _pools(self, k_pool, v_pool, dtype, shape, stream):
+        """Checks the pools and the current device; returns the stream's handle."""
         if self._current() != self._index:
             raise ValueError("the current device is not %s" % self.device)
-        _expect("k_pool", k_pool, self.device, dtypes, shape)
-        _expect("v_pool", v_pool, self.device, dtypes, shape)
+        _expect("k_pool", k_pool, self._index, dtype, shape)
+        _expect("v_pool", v_pool, self._index, dtype, shape)
+        return self._raw_stream(self._index) if stream is None else _stream(stream)
 
     def _write(self, call, k_pool, v_pool, q, q_out, k_new, v_new, q_weight, k_weight, eps, stream) -> None:
-        rows = _fresh_rows(self.shape, self.batch, self.device, q, q_out, k_new, v_new, q_weight, k_weight, eps)
-        _check(call(ctypes.byref(self._cfg), ctypes.byref(self._desc), _dev(k_pool), _dev(v_pool), ctypes.byref(rows), _stream(stream)))
+        rows = _fresh_rows(self.shape, self.batch, self._index, q, q_out, k_new, v_new, q_weight, k_weight, eps)
+        _check(call(*self._args, k_pool.data_ptr(), v_pool.data_ptr(), ctypes.byref(rows), stream))
 
     def write(self, k_pool, v_pool, q, q_out, k_new, v_new, q_weight=None, k_weight=None, eps: float = 1e-6, stream=None) -> None:
         """The new tokens' un-rotated rows: q (normalised with q_weight, rotated) to q_out, k (likewise) and v to their slots.  q, k_new and v_new
         may be slices [batch, heads, D] of a fused projection; q None: keys and values alone."""
-        self._pools(k_pool, v_pool, _BF16, self._pool)
-        self._write(_lib.tessera_decode_write, k_pool, v_pool, q, q_out, k_new, v_new, q_weight, k_weight, eps, stream)
+        st = self._pools(k_pool, v_pool, self._bf16, self._pool, stream)
+        self._write(_lib.tessera_decode_write, k_pool, v_pool, q, q_out, k_new, v_new, q_weight, k_weight, eps, st)
 
     def write_kv4(self, k_pool4, v_pool4, q, q_out, k_new, v_new, q_weight=None, k_weight=None, eps: float = 1e-6, stream=None) -> None:
         """write() into 4-bit pools (pool4_shape)."""
-        self._pools(k_pool4, v_pool4, _BYTES, self._pool4)
-        self._write(_lib.tessera_decode_write_kv4, k_pool4, v_pool4, q, q_out, k_new, v_new, q_weight, k_weight, eps, stream)
+        st = self._pools(k_pool4, v_pool4, self._u8, self._pool4, stream)
+        self._write(_lib.tessera_decode_write_kv4, k_pool4, v_pool4, q, q_out, k_new, v_new, q_weight, k_weight, eps, st)
 
     def _attn(self, call, k_pool, v_pool, q, out, lse, stream) -> None:
-        _expect("q", q, self.device, _BF16, self._q)
-        _expect("out", out, self.device, _BF16, self._q)
+        _expect("q", q, self._index, self._bf16, self._q)
+        _expect("out", out, self._index, self._bf16, self._q)
         if lse is not None:
-            _expect("lse", lse, self.device, _F32, self._q[:2])
-        _check(call(ctypes.byref(self._cfg), ctypes.byref(self._desc), _dev(k_pool), _dev(v_pool), _dev(q), _dev(out), _dev(lse),
-                    _dev(self.workspace), self.workspace.numel(), _stream(stream)))
+            _expect("lse", lse, self._index, self._f32, self._lse)
+        _check(call(*self._args, k_pool.data_ptr(), v_pool.data_ptr(), q.data_ptr(), out.data_ptr(), _dev(lse), self.workspace.data_ptr(),
+                    self.workspace.numel(), stream))
 
     def attn(self, k_pool, v_pool, q, out, lse=None, stream=None) -> None:
         """Attention of the rotated q [batch, H_q, D] over the requests' 16-bit pages."""
-        self._pools(k_pool, v_pool, _BF16, self._pool)
-        self._attn(_lib.tessera_decode_attn, k_pool, v_pool, q, out, lse, stream)
+        st = self._pools(k_pool, v_pool, self._bf16, self._pool, stream)
+        self._attn(_lib.tessera_decode_attn, k_pool, v_pool, q, out, lse, st)
 
     def attn_kv4(self, k_pool4, v_pool4, q, out, lse=None, stream=None) -> None:
         """Attention of the rotated q [batch, H_q, D] over the requests' 4-bit pages (pool4_shape)."""
-        self._pools(k_pool4, v_pool4, _BYTES, self._pool4)
-        self._attn(_lib.tessera_decode_attn_kv4, k_pool4, v_pool4, q, out, lse, stream)
+        st = self._pools(k_pool4, v_pool4, self._u8, self._pool4, stream)
+        self._attn(_lib.tessera_decode_attn_kv4, k_pool4, v_pool4, q, out, lse, st)
 
 
 def selftest_bounded_wait(max_cycles: int, stream=None):

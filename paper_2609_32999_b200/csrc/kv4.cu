@@ -67,9 +67,17 @@ kv4_kernel(const uint8_t *__restrict__ k_src, const uint8_t *__restrict__ v_src,
     if constexpr (TO_4BIT) {
         const uint4 *k = reinterpret_cast<const uint4 *>(k_src) + o16, *v = reinterpret_cast<const uint4 *>(v_src) + o16;
         uint8_t *kd = k_dst + oc, *vd = v_dst + oc, *kn = k_dst + on, *vn = v_dst + on;
-        for (int h = h0; h < H_kv; h += step, k += step * (D / 8), v += step * (D / 8)) {
-            uint4 klo = ldg_stream(k), khi = ldg_stream(k + HALF);
-            const uint4 vlo = ldg_stream(v), vhi = ldg_stream(v + HALF);
+        // The next head is on its way while one is worked on, but for keys that are rotated as well (72 000 rows: 79.5 -> 74.8 us,
+        // rotated 90.7 -> 93.8, for want of registers).
+        constexpr bool kAhead = !ROTATE;
+        uint4 klo, khi, vlo, vhi, next[4];
+        auto load = [&](uint4 &a, uint4 &b, uint4 &x, uint4 &y) { a = ldg_stream(k), b = ldg_stream(k + HALF), x = ldg_stream(v), y = ldg_stream(v + HALF); };
+        if (kAhead && h0 < H_kv) load(next[0], next[1], next[2], next[3]);
+        for (int h = h0; h < H_kv; h += step) {
+            if (kAhead) klo = next[0], khi = next[1], vlo = next[2], vhi = next[3];
+            else load(klo, khi, vlo, vhi);
+            k += step * (D / 8), v += step * (D / 8);
+            if (kAhead && h + step < H_kv) load(next[0], next[1], next[2], next[3]);
             if (ROTATE) {
                 float lo[8], hi[8];
                 unpack_bf16x8(klo, lo);
