@@ -172,8 +172,7 @@ def _expect(what: str, t, index: int, dtype, shape, rows: bool = False) -> None:
         raise ValueError("%s: strides %s" % (what, tuple(t.stride())))
 
 
-def _fresh_rows(sh, n: int, index: int, q, q_out, k, v, q_weight, k_weight, eps) -> FreshRows:
-    from torch import bfloat16
+def _fresh_rows(sh, n: int, index: int, bfloat16, q, q_out, k, v, q_weight, k_weight, eps) -> FreshRows:
     hq, h, d = sh.num_q_heads, sh.num_kv_heads, sh.head_dim
     if q is not None:
         _expect("q", q, index, bfloat16, (n, hq, d), rows=True)
@@ -291,7 +290,8 @@ class Plan:
                           v_cache=None, stream=None) -> None:
         """extend_write with per-head norms of q and k before the rotation, q written to q_out (q itself, or another tensor); q, k_new_raw and
         v_new may be slices [n_q, heads, D] of a fused projection.  q None: keys and values alone."""
-        rows = _fresh_rows(self.shape, int(self.info.n_q), k_new_raw.get_device(), q, q_out, k_new_raw, v_new, q_weight, k_weight, eps)
+        from torch import bfloat16
+        rows = _fresh_rows(self.shape, int(self.info.n_q), k_new_raw.get_device(), bfloat16, q, q_out, k_new_raw, v_new, q_weight, k_weight, eps)
         _check(_lib.tessera_extend_write_norm(self._h, _dev(k_pool), _dev(v_pool), ctypes.byref(rows), _dev(k_cache), _dev(v_cache), _stream(stream)))
 
     def partial_prefill_attn(self, k_pool, v_pool, q, k_new, v_new, out, lse=None, stream=None) -> None:
@@ -387,7 +387,7 @@ class Decode:
         return self._raw_stream(self._index) if stream is None else _stream(stream)
 
     def _write(self, call, k_pool, v_pool, q, q_out, k_new, v_new, q_weight, k_weight, eps, stream) -> None:
-        rows = _fresh_rows(self.shape, self.batch, self._index, q, q_out, k_new, v_new, q_weight, k_weight, eps)
+        rows = _fresh_rows(self.shape, self.batch, self._index, self._bf16, q, q_out, k_new, v_new, q_weight, k_weight, eps)
         _check(call(*self._args, k_pool.data_ptr(), v_pool.data_ptr(), ctypes.byref(rows), stream))
 
     def write(self, k_pool, v_pool, q, q_out, k_new, v_new, q_weight=None, k_weight=None, eps: float = 1e-6, stream=None) -> None:

@@ -113,6 +113,8 @@ struct Item {
     AttnTile t0, t1;
     int n_tiles, step0, n_steps0, n_steps1, n_steps, T, req_pages;
     const int32_t *bt;
+    // With a window a tile leaves out skip0, respectively skip1, of the item's steps, from step `sinks` on.
+    int sinks, skip0, skip1;
 };
 
 // The block's first item, as the descriptor tables have it: brought to shared memory while the launch still waits for its
@@ -185,8 +187,20 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
         it.T = it.wk.seq_len;
         it.req_pages = (it.T + page_size - 1) / page_size;
         it.bt = pages + it.wk.page_begin;
+        if constexpr (W) {
+            it.sinks = max((int)(((uint32_t)n_sink + kStep - 1) / kStep) - it.step0, 0);
+            auto skip = [&](int kv_full, int n) { return min(max(max(kv_full - window, 0) / kStep - it.wk.gap - it.step0 - it.sinks, 0), max(n - it.sinks, 0)); };
+            it.skip0 = skip(it.t0.kv_full, it.n_steps0);
+            it.skip1 = skip(it.t1.kv_full, it.n_steps1);
+        }
         return it;
     };
+    // Whether tile q has step j of the item, how many of its steps come before that, how many it has.
+    auto has_step = [](const Item &it, int q, int j) {
+        return j < (q ? it.n_steps1 : it.n_steps0) && (!W || j < it.sinks || j >= it.sinks + (q ? it.skip1 : it.skip0));
+    };
+    auto nth_step = [](const Item &it, int q, int j) { return !W || j < it.sinks ? j : j - (q ? it.skip1 : it.skip0); };
+    auto count_steps = [](const Item &it, int q) { return (q ? it.n_steps1 : it.n_steps0) - (!W ? 0 : q ? it.skip1 : it.skip0); };
     // the 128-key step of the request that step v of the item's count is
     auto real_step = [](const Item &it, int v) { return W && v >= it.wk.sink_steps ? v + it.wk.gap : v; };
     // block-table index of the page that lane `lane` brings of the steps from v on (32 pages)
@@ -348,6 +362,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
             const int n_steps = it.n_steps;
             const int my_steps = q ? it.n_steps1 : it.n_steps0;
             const int T = it.T, step0 = it.step0;
+            // the tile's last step
+            const int last_s = W && (q ? it.skip1 : it.skip0) > 0 && it.sinks + (q ? it.skip1 : it.skip0) == my_steps ? it.sinks - 1 : my_steps - 1;
             const int tail_step = (T % kStep) ? T / kStep - step0 - (W ? it.wk.gap : 0) : -1;   // step holding slots past the sequence end
 
             auto ring_wait = [&](int item, int code) {
@@ -375,7 +391,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                 }
                 umma_commit(smem_u32(&bars.s_full[q]));
                 umma_commit(smem_u32(&bars.empty[slot_of(2 * j)]));    // K_j no longer needed by this tile
-                if (j == my_steps - 1) umma_commit(smem_u32(&bars.q_empty[q]));   // the item's last read of Q
+                if (j == last_s) umma_commit(smem_u32(&bars.q_empty[q]));   // the item's last read of Q
             };
 
             ring_wait(0, 3);
@@ -383,6 +399,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                 mbar_wait(smem_u32(&bars.q_full[q]), q_uses & 1, abort_flag, status, 4);
                 ++q_uses;
                 tc_fence_after();
+            }
+            if (has_step(it, q, 0)) {
                 if (lane == 0) issue_s(0);
             } else if (lane == 0) {
                 mbar_arrive(smem_u32(&bars.empty[slot_of(0)]));
@@ -392,12 +410,13 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                 ring_wait(2 * j + 1, 5);                               // V_j
                 const int vslot = slot_of(2 * j + 1);
                 const bool more = j + 1 < n_steps;
-                if (j >= my_steps) {
-                    // this tile is finished or absent: only release the slots
+                if (!has_step(it, q, j)) {
+                    // this tile is finished or absent (or sees nothing here): only release the slots
                     if (more) ring_wait(2 * j + 2, 3);
                     if (lane == 0) {
                         mbar_arrive(smem_u32(&bars.empty[vslot]));
-                        if (more) mbar_arrive(smem_u32(&bars.empty[slot_of(2 * j + 2)]));
+                        if (W && more && has_step(it, q, j + 1)) issue_s(j + 1);
+                        else if (more) mbar_arrive(smem_u32(&bars.empty[slot_of(2 * j + 2)]));
                     }
                     __syncwarp();
                     continue;
@@ -436,23 +455,24 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                         __syncwarp();
                     }
                 }
-                const bool next_s = j + 1 < my_steps;
+                const bool next_s = W ? has_step(it, q, j + 1) : j + 1 < my_steps;
+                const int nth = nth_step(it, q, j);
                 if (more) ring_wait(2 * j + 2, 3);                     // K_{j+1}
                 const uint32_t vbase = smem_u32(sm + kSmemRing + vslot * kSlotBytes);
                 // P arrives in two halves: P.V of the first 64 keys runs while the softmax warps are still
                 // on the exponentials of the other 64
-                mbar_wait(smem_u32(&bars.p_half[q][0]), (step_base + j) & 1, abort_flag, status, 6);
+                mbar_wait(smem_u32(&bars.p_half[q][0]), (step_base + nth) & 1, abort_flag, status, 6);
                 tc_fence_after();
                 if (lane == 0) {
 #pragma unroll
                     for (int k = 0; k < kStep / 32; ++k) {
                         const uint64_t b = smem_desc_sw128(vbase + k * 2048, kHalfBytes, 1024);
-                        umma_ts(tO, tS + k * 8, b, idesc_o, (j > 0) || (k > 0));   // P of keys [16k, 16k + 16): columns 8k .. 8k + 7
+                        umma_ts(tO, tS + k * 8, b, idesc_o, (nth > 0) || (k > 0));   // P of keys [16k, 16k + 16): columns 8k .. 8k + 7
                     }
                     umma_commit(smem_u32(&bars.pv_half[q]));
                 }
                 __syncwarp();
-                mbar_wait(smem_u32(&bars.p_half[q][1]), (step_base + j) & 1, abort_flag, status, 11);
+                mbar_wait(smem_u32(&bars.p_half[q][1]), (step_base + nth) & 1, abort_flag, status, 11);
                 tc_fence_after();
                 if (lane == 0) {
 #pragma unroll
@@ -468,7 +488,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                 __syncwarp();
             }
             ring_base += 2 * n_steps;
-            step_base += my_steps;
+            step_base += count_steps(it, q);
         }
     }
     } else {
@@ -502,7 +522,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
         if (w < 0) continue;
         const Item it = load_item(w, round == 0);
         if (it.n_tiles == 0) break;
-        const int n_tiles = it.n_tiles, n_steps = it.n_steps, n_steps0 = it.n_steps0, n_steps1 = it.n_steps1;
+        const int n_tiles = it.n_tiles, n_steps = it.n_steps;
         const int step0 = it.step0, kvh = it.wk.kvh;
         const AttnTile &t0 = it.t0, &t1 = it.t1;
         int p_row[2][2];
@@ -520,15 +540,36 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
         for (int j = 0; j < n_steps; ++j) {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                if (q >= n_tiles || j >= (q ? n_steps1 : n_steps0)) continue;
+                if (q >= n_tiles || !has_step(it, q, j)) continue;
                 const uint32_t tS = tmem + kTmemS + q * 128 + lane_base;
-                const int par = (step_base[q] + j) & 1;
+                const int nth = nth_step(it, q, j), par = (step_base[q] + nth) & 1;
                 // S_j complete; this also means P.V of step j-1 has completed (it was issued earlier)
                 mbar_wait(smem_u32(&bars.s_full[q]), par, abort_flag, status, 7);
                 tc_fence_after();
                 const int key0 = real_step(it, step0 + j) * kStep;
-                bool masked = key0 + kStep > (q ? t1.kv_full : t0.kv_full);   // a causal limit falls in this step
-                if constexpr (W) masked = masked || (key0 < (q ? t1.kv_len : t0.kv_len) - window && key0 + kStep > n_sink);   // or a window's
+                // a causal limit falls in this step, or a window's (for each warp's rows by themselves, whose positions ascend)
+                bool masked, below = false;
+                if constexpr (W) {
+                    const int p_first = __shfl_sync(0xffffffffu, p_row[q][0], 0), p_last = __shfl_sync(0xffffffffu, p_row[q][1], 31);
+                    if (key0 > p_last || (key0 + kStep <= p_first - window + 1 && key0 >= n_sink)) {
+                        // the warp's rows see none of these keys
+                        uint32_t none[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) none[k] = 0u;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            tmem_st_16x128b_x8(tS + 32 * h, none);
+                            tmem_wait_st();
+                            tc_fence_before();
+                            mbar_arrive(smem_u32(&bars.p_half[q][h]));
+                        }
+                        continue;
+                    }
+                    masked = key0 + kStep > p_first + 1;
+                    below = key0 <= p_last - window && key0 + kStep > n_sink;
+                } else {
+                    masked = key0 + kStep > (q ? t1.kv_full : t0.kv_full);
+                }
 
                 // The thread's 2 x 64 scores (rows t/4 and t/4 + 8 of the warp's 16; of every group of 8
                 // columns, columns 2 (t%4) and 2 (t%4) + 1) stay in registers for the whole step.
@@ -540,10 +581,16 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                     for (int k = 0; k < 16; ++k)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                        {
-                            const int key = key0 + 8 * k + cq + (e & 1), p = p_row[q][e >> 1];
-                            if (key > p || (W && key >= n_sink && key <= p - window)) s[4 * k + e] = 0xff800000u;   // -inf
-                        }
+                            if (key0 + 8 * k + cq + (e & 1) > p_row[q][e >> 1]) s[4 * k + e] = 0xff800000u;   // -inf
+                }
+                if (W && below) {
+                    // of the columns from n_sink on, those up to p - window
+                    const int col0 = n_sink - key0, top[2] = {p_row[q][0] - window - key0, p_row[q][1] - window - key0};
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (8 * k + cq + (e & 1) >= col0 && 8 * k + cq + (e & 1) <= top[e >> 1]) s[4 * k + e] = 0xff800000u;
                 }
                 uint32_t pk[16];
                 // Probabilities of column groups [8 h, 8 h + 8) (keys [64 h, 64 h + 64)) against the current
@@ -613,7 +660,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                 // after each half: once the first half has been released, a refresh concerns only the
                 // second half (the first half's P.V is brought to the new reference with the accumulator).
                 float sum_a[2], sum_b[2], factor[2];
-                bool fresh = j == 0;
+                bool fresh = nth == 0;
                 // (a row whose first keys are still to come has no reference yet: the one it starts with may be far off)
                 if constexpr (W) fresh = fresh || __any_sync(0xffffffffu, m_row[q][0] == -INFINITY || m_row[q][1] == -INFINITY);
                 if (!fresh) {
@@ -621,7 +668,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                     fresh = __any_sync(0xffffffffu, !(sum_a[0] <= 64.f && sum_a[1] <= 64.f));
                 }
                 if (fresh) {
-                    refresh(j > 0, factor);       // S_j complete means P.V of step j - 1 has completed: O is at rest
+                    refresh(nth > 0, factor);     // S_j complete means P.V of step j - 1 has completed: O is at rest
                     exp_half(0, sum_a);
                     l_row[q][0] *= factor[0];
                     l_row[q][1] *= factor[1];
@@ -650,7 +697,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
         // accumulators are not touched before they have been read here.
         for (int q = 0; q < n_tiles; ++q) {
             const AttnTile &t = q ? t1 : t0;
-            const int my_steps = q ? n_steps1 : n_steps0;
+            const int my_steps = count_steps(it, q);
             mbar_wait(smem_u32(&bars.pv_done[q]), (step_base[q] + my_steps - 1) & 1, abort_flag, status, 9);
             tc_fence_after();
             const float l_tot[2] = {quad_sum(l_row[q][0]), quad_sum(l_row[q][1])};
@@ -730,8 +777,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                     lse[(size_t)(t.q_begin + row_tok[rr]) * H_q + kvh * g + row_head[rr]] =
                         (m_row[q][rr] + log2f(l_tot[rr])) * 0.6931471805599453f;
         }
-        step_base[0] += n_steps0;
-        step_base[1] += n_steps1;
+        step_base[0] += count_steps(it, 0);
+        step_base[1] += count_steps(it, 1);
         }
     }
 

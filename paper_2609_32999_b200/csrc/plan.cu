@@ -39,8 +39,6 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
     if (window < 0 || n_sink < 0) return fail(TESSERA_INVALID_ARG, "negative window or sink count");
     window = std::min(window, 1 << 30);        // (more than any pool holds; sums and differences of it and a position stay in 32 bits)
     n_sink = window > 0 ? std::min(n_sink, 1 << 30) : 0;
-    pl->window = window;
-    pl->n_sink = n_sink;
     if (d->batch < 0 || num_pool_pages < 0 || d->n_free < 0)
         return fail(TESSERA_INVALID_ARG, "negative batch, pool size or free-list length");
     if (d->batch > 0 && (!d->seq_len || !d->unit_off || !d->recompute_off))
@@ -73,6 +71,9 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
     pl->batch = d->batch;
 
     const int batch = d->batch;
+    if (batch > 0 && window >= *std::max_element(d->seq_len, d->seq_len + batch)) window = n_sink = 0;      // it reaches over every prompt
+    pl->window = window;
+    pl->n_sink = n_sink;
     // ---- CSR sanity
     if (batch > 0) {
         if (d->unit_off[0] != 0 || d->recompute_off[0] != 0) return fail(TESSERA_INVALID_ARG, "CSR offsets must start at 0");
@@ -369,24 +370,39 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
             return window > 0 ? std::max(0, std::max(0, pl->tiles[tile].kv_full - window) / page - sink_steps) : 0;
         };
         auto steps_of = [&](int32_t tile) { return (pl->tiles[tile].kv_len + page - 1) / page - gap[tile]; };
+        // Of the steps [b, e) of its item a tile has those before its end and, with a window, among the sinks or from its first
+        // row's window on.
+        auto from_of = [&](int32_t tile) { return window > 0 ? std::max(sink_steps, std::max(0, pl->tiles[tile].kv_full - window) / page - gap[tile]) : 0; };
+        struct Steps { int a, b, both; };          // of tile a, of tile b, of both
+        auto steps_in = [&](int32_t ta, int32_t tb, int b, int e) -> Steps {
+            auto count = [&](int end, int from) {
+                if (window == 0) return std::max(0, std::min(e, end) - b);
+                return std::max(0, std::min({e, end, sink_steps}) - b) + std::max(0, std::min(e, end) - std::max(b, from));
+            };
+            Steps s{count(steps_of(ta), from_of(ta)), 0, 0};
+            if (tb >= 0) {
+                s.b = count(steps_of(tb), from_of(tb));
+                s.both = count(std::min(steps_of(ta), steps_of(tb)), std::max(from_of(ta), from_of(tb)));
+            }
+            return s;
+        };
         // Modelled cycles of an item (clock64 on a B200): item fetch 1 700, epilogue and what the first step takes
         // longer than a later one 4 700 per tile, 3 180 per step of both tiles, 2 400 per step of a lone one (whose
         // softmax and MMAs wait for each other).
-        auto model_cycles = [](int steps_a, int steps_b, int n_tiles) -> int64_t {
-            const int both = std::min(steps_a, steps_b), single = std::max(steps_a, steps_b) - both;
-            return 1700 + (int64_t)n_tiles * 4700 + (int64_t)both * 3180 + (int64_t)single * 2400;
+        auto model_cycles = [](const Steps &s) -> int64_t {
+            return 1700 + (int64_t)((s.a > 0) + (s.b > 0)) * 4700 + (int64_t)s.both * 3180 + (int64_t)(s.a + s.b - 2 * s.both) * 2400;
         };
-        // Consecutive tiles of a request pair up.  With a window they do where the model gives the pair no more cycles than
-        // two items: tile b also walks the steps that only tile a sees, which rows scattered over a long prompt have many of.
+        // Consecutive tiles of a request pair up.  With a window they do where no keys between them are nobody's and the model gives
+        // the pair no more cycles than two items.
         for (size_t k = 0; k < pl->tiles.size();) {
             const int32_t a = (int32_t)k, b2 = k + 1 < pl->tiles.size() && pl->tiles[k + 1].req == pl->tiles[k].req ? a + 1 : -1;
             gap[a] = gap_at(a);
             bool together = b2 >= 0 && (window == 0 || pl->tiles[b2].kv_full - window <= pl->tiles[a].kv_len);
             if (together && window > 0) {
                 gap[b2] = gap_at(b2);
-                const int64_t apart = model_cycles(0, steps_of(a), 1) + model_cycles(0, steps_of(b2), 1);
+                const int64_t apart = model_cycles(steps_in(a, -1, 0, steps_of(a))) + model_cycles(steps_in(b2, -1, 0, steps_of(b2)));
                 gap[b2] = gap[a];
-                together = model_cycles(steps_of(a), steps_of(b2), 2) <= apart;
+                together = model_cycles(steps_in(a, b2, 0, steps_of(b2))) <= apart;
             }
             pairs.push_back({a, together ? b2 : -1});
             k += together ? 2 : 1;
@@ -422,14 +438,15 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
             part_cost.clear();          // of the parts of one head; every head has the same
             int64_t slots = 0, sum = 0, top = 0;
             for (auto &pr : pairs) {
-                const int sl = long_steps(pr), sa = pr.second >= 0 ? steps_of(pr.first) : 0, parts = parts_of(sl, limit);
+                const int sl = long_steps(pr), parts = parts_of(sl, limit);
                 const int len = (sl + parts - 1) / parts;
                 for (int b0 = 0; b0 < sl; b0 += len) {
-                    const int n_b = std::min(sl, b0 + len) - b0, n_a = std::max(0, std::min(sa, b0 + len) - b0);
-                    part_cost.push_back(model_cycles(n_a, n_b, n_a > 0 ? 2 : 1));
+                    const Steps n = steps_in(pr.first, pr.second, b0, std::min(sl, b0 + len));
+                    if (n.a + n.b == 0) continue;
+                    part_cost.push_back(model_cycles(n));
                     sum += part_cost.back() * Hkv;
                     top = std::max(top, part_cost.back());
-                    if (parts > 1) slots += (n_a > 0 ? 2 : 1) * Hkv;
+                    if (parts > 1) slots += ((n.a > 0) + (n.b > 0)) * Hkv;
                 }
             }
             const bool one_round = (int64_t)part_cost.size() * Hkv <= num_sms;
@@ -462,8 +479,7 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
             if (modelled(l, INT64_MAX) < modelled(longest, INT64_MAX) * 90 / 100) limit = l;
         } else if (uncut > 0 && uncut <= (int64_t)kSplitMaxRounds * num_sms) {
             int64_t all = 0;
-            for (auto &pr : pairs)
-                all += Hkv * model_cycles(pr.second >= 0 ? steps_of(pr.first) : 0, long_steps(pr), pr.second >= 0 ? 2 : 1);
+            for (auto &pr : pairs) all += Hkv * model_cycles(steps_in(pr.first, pr.second, 0, long_steps(pr)));
             int64_t best = modelled(longest, INT64_MAX) * 90 / 100;
             if (best > all / num_sms)           // otherwise no cut can reach it
                 for (int l = longest * 3 / 4; l >= 2 * kSplitMinSteps && items_at(l) <= 2 * kSplitMaxRounds * num_sms; l = l * 5 / 6) {
@@ -475,36 +491,40 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
         pl->n_slots = 0;
         for (auto &pr : pairs) {
             const int32_t a = pr.first, b2 = pr.second;
-            const int sa = steps_of(a), sl = long_steps(pr);                   // sa <= sl: positions ascend
+            const int sl = long_steps(pr);
             const int parts = parts_of(sl, limit), len = (sl + parts - 1) / parts;
-            const int parts_b = (sl + len - 1) / len, parts_a = b2 >= 0 ? (sa + len - 1) / len : parts_b;
+            int parts_a = 0, parts_b = 0;          // parts in which the tiles have steps
+            for (int sb = 0; sb < sl; sb += len) {
+                const Steps n = steps_in(a, b2, sb, std::min(sl, sb + len));
+                parts_a += n.a > 0;
+                parts_b += n.b > 0;
+            }
             for (int h = 0; h < Hkv; ++h) {
                 if (parts == 1) {
                     pl->work.push_back({a, b2, h, 0, sl, -1, -1, 0, 0, 0, 0, 0});
                     continue;
                 }
                 const int32_t slot_a = pl->n_slots, slot_b = slot_a + parts_a;
-                for (int p2 = 0; p2 < parts_b; ++p2) {
-                    const int sb = p2 * len, se = std::min(sl, sb + len);
-                    if (p2 < parts_a) pl->work.push_back({a, b2, h, sb, se, slot_a + p2, b2 >= 0 ? slot_b + p2 : -1, 0, 0, 0, 0, 0});
-                    else pl->work.push_back({b2, -1, h, sb, se, slot_b + p2, -1, 0, 0, 0, 0, 0});   // tile a is already finished
+                int32_t next_a = slot_a, next_b = slot_b;
+                for (int sb = 0; sb < sl; sb += len) {
+                    const int se = std::min(sl, sb + len);
+                    const Steps n = steps_in(a, b2, sb, se);
+                    if (n.a > 0 && n.b > 0) pl->work.push_back({a, b2, h, sb, se, next_a++, next_b++, 0, 0, 0, 0, 0});
+                    else if (n.a > 0) pl->work.push_back({a, -1, h, sb, se, next_a++, -1, 0, 0, 0, 0, 0});
+                    else if (n.b > 0) pl->work.push_back({b2, -1, h, sb, se, next_b++, -1, 0, 0, 0, 0, 0});   // tile a is already finished
                 }
                 const AttnTile &ta = pl->tiles[a], &tb = pl->tiles[b2 >= 0 ? b2 : a];
                 pl->combine.push_back({a, h, parts_a, slot_a, ta.q_begin, ta.n_tok, 0, 0});
                 if (b2 >= 0) pl->combine.push_back({b2, h, parts_b, slot_b, tb.q_begin, tb.n_tok, 0, 0});
-                pl->n_slots += parts_a + (b2 >= 0 ? parts_b : 0);
+                pl->n_slots += parts_a + parts_b;
             }
         }
-        auto cycles_of = [&](const AttnWork &w) {
-            const int sa = std::min(w.step_end, steps_of(w.tile_a)) - w.step_begin;
-            const int sb = w.tile_b >= 0 ? std::min(w.step_end, steps_of(w.tile_b)) - w.step_begin : 0;
-            return model_cycles(sa, sb, w.tile_b >= 0 ? 2 : 1);
-        };
+        auto steps_of_item = [&](const AttnWork &w) { return steps_in(w.tile_a, w.tile_b, w.step_begin, w.step_end); };
+        auto cycles_of = [&](const AttnWork &w) { return model_cycles(steps_of_item(w)); };
         // cost of an item = its (tile, 128-key step) count, kept in the item for the sorts
         for (AttnWork &w : pl->work) {
-            int c = std::min(w.step_end, steps_of(w.tile_a)) - w.step_begin;
-            if (w.tile_b >= 0) c += std::min(w.step_end, steps_of(w.tile_b)) - w.step_begin;
-            w.cost = c;
+            const Steps n = steps_of_item(w);
+            w.cost = n.a + n.b;
             const int32_t req = pl->tiles[w.tile_a].req;
             w.seq_len = pl->seq_len[req];
             w.page_begin = pl->page_off[req];
