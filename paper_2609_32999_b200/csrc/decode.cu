@@ -189,12 +189,16 @@ __device__ __forceinline__ void empty_requests(const Args &a) {
         }
 }
 
-// SMALL: pages of fewer tokens than a tile.
-template <int D, bool F4, int NQ, bool SMALL>
+// SMALL: pages of fewer tokens than a tile.  FOLD (4-bit, at most 4 queries a KV head): columns 4 to 7 hold the same queries as 0 to
+// 3, and stand for the tile's second 16 keys where 0 to 3 stand for the first: a lane has half the scores to turn into weights, none
+// of them of an empty column.  The two sets of columns, each with a reference of its own, come together when the pair ends.
+template <int D, bool F4, int NQ, bool SMALL, bool FOLD>
 __global__ void __launch_bounds__(Geo<D, F4, NQ>::kThreads, 1)
 decode_attn_kernel(const __grid_constant__ Args a) {
     using G = Geo<D, F4, NQ>;
     constexpr int T = G::kTile, SUB = T / 16, NW = G::kWarps, NT = G::kThreads, CPR = G::kRow / 16, Q8 = 8 * NQ, KS = D / 16, RP = D + 4;
+    constexpr int SC = FOLD ? 1 : SUB;                // sets of 16 keys that a lane has scores of
+    static_assert(!FOLD || (F4 && NQ == 1 && SUB == 2), "");
     constexpr uint32_t kAllRows = T == 32 ? 0xffffffffu : 0xffffu;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint2 s_stage[NW][G::kStages];         // rows that are there (bit i: row i) and flags
@@ -236,6 +240,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
         const uint32_t head_bytes = F4 ? (uint32_t)a.page_size * (D / 2 + 8) : (uint32_t)G::kRow;
         const uint32_t row_bytes = F4 ? (uint32_t)G::kRow : a.H_kv * head_bytes, page_bytes = F4 ? a.H_kv * head_bytes : row_bytes << page_shift;
         const uint32_t numbers = (uint32_t)a.page_size * (D / 2);
+        int run = 0;                               // tiles from j on that are neither first nor last of their pair and all there, pages apart
         auto fetch = [&](int at) {
             if (sent < my_tiles) {
                 const int key0 = tile_at(j) * T;
@@ -244,6 +249,9 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                 auto page_of = [&](int row) { return __shfl_sync(0xffffffffu, page_ids, SMALL ? (j - jb) * GROUPS + row / 8 : j - jb); };
                 const int page = page_of(lane & (T - 1));
                 uint32_t rows = kAllRows;
+                if (run > 0 && in_pool(page)) {
+                    if (lane == 0) s_stage[warp][at] = make_uint2(kAllRows, 0u);
+                } else {
                 if (SMALL || !(in_pool(page) && key0 + T <= vis.len && (key0 >= vis.first || key0 + T <= vis.sinks))) {
                     const int key = key0 + (lane & (T - 1));
                     rows = __ballot_sync(0xffffffffu, key < vis.len && (key < vis.sinks || key >= vis.first) && in_pool(page)) & kAllRows;
@@ -251,6 +259,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                 if (lane == 0) {
                     s_stage[warp][at] = make_uint2(rows, (j == 0 ? kFirst : 0u) | (j == vis.n - 1 ? kLast : 0u));
                     if (j == 0 || sent == 0) s_pair[warp][at] = {r * a.H_kv + h, base + h * vis.n, vis.n};
+                }
                 }
                 const uint32_t kb = ring + at * G::kStageBytes, vb = kb + T * G::kRow;
                 auto copy = [&](auto all_there) {
@@ -277,8 +286,10 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                 };
                 if (rows == kAllRows) copy(std::true_type{});
                 else copy(std::false_type{});
-                if (++sent < my_tiles) {
-                    if (++j == vis.n) {
+                ++sent, ++j;
+                if (--run > 0) {
+                } else if (sent < my_tiles) {
+                    if (j == vis.n) {
                         const bool same = jb == 0 && h + 1 < a.H_kv;          // the next head's pages are the ones at hand
                         j = jb = 0;
                         if (++h == a.H_kv) {
@@ -293,6 +304,8 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                         jb = j;
                         load_pages();
                     }
+                    if (!SMALL && j > 0 && (j + 1 < vis.front || j > vis.front || vis.first == 0))
+                        run = min(min(vis.n - 1, jb + kBatch), vis.first > 0 && j < vis.front ? vis.front - 1 : vis.n) - j;
                 }
             }
             cp_commit();
@@ -304,13 +317,13 @@ decode_attn_kernel(const __grid_constant__ Args a) {
         float unit[NQ][2];               // score times scale log2(e) per score sum: scale_log2, 4-bit: by column, for q's and the codes' scaling
         float m[NQ][2], l[NQ][2], off[NQ][2][2];         // off (4-bit): sums of p times a half's middle value
         float acc[NQ][D / 16][4];        // 4-bit: times v_unit 2^-133, second half 2^-129
-        float v_unit = kValueUnit;
+        float v_unit = kValueUnit, v_limit = kValueTop / kValueUnit;
 
         auto begin_pair = [&](int pair) {
             const int qr = pair / a.H_kv, qh = pair - qr * a.H_kv;
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
-                const int col = n * 8 + quad;
+                const int col = n * 8 + (FOLD ? quad & 3 : quad);
                 const bool there = col < a.g;
                 const __nv_bfloat16 *q = a.q + ((size_t)qr * a.H_q + qh * a.g + (there ? col : 0)) * D;
                 if constexpr (F4) {
@@ -371,7 +384,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                         for (int i = 0; i < 2; ++i) qf[n][s][i] = there ? *reinterpret_cast<const uint32_t *>(q + 16 * s + 8 * i + 2 * t) : 0u;
                     unit[n][0] = unit[n][1] = a.scale_log2;
                 }
-                v_unit = kValueUnit;
+                v_unit = kValueUnit, v_limit = kValueTop / kValueUnit;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) m[n][e] = -INFINITY, l[n][e] = off[n][0][e] = off[n][1][e] = 0.f;
 #pragma unroll
@@ -382,6 +395,19 @@ decode_attn_kernel(const __grid_constant__ Args a) {
         };
         // Sums over the lanes of a column, and (4-bit) the middle values' share into the accumulators.
         auto sum_up = [&]() {
+            if constexpr (FOLD) {              // columns c and c + 4 (lanes t and t + 2) to one reference, and together
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float ref = fmaxf(m[0][e], __shfl_xor_sync(0xffffffffu, m[0][e], 2)), f = m[0][e] == -INFINITY ? 0.f : ex2(m[0][e] - ref);
+                    m[0][e] = ref;
+                    auto both = [&](float x) { return x * f + __shfl_xor_sync(0xffffffffu, x * f, 2); };
+                    l[0][e] = both(l[0][e]);
+                    off[0][0][e] = both(off[0][0][e]);
+                    off[0][1][e] = both(off[0][1][e]);
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d) acc[0][d][e] = both(acc[0][d][e]), acc[0][d][e + 2] = both(acc[0][d][e + 2]);
+                }
+            }
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -481,15 +507,17 @@ decode_attn_kernel(const __grid_constant__ Args a) {
             const uint8_t *kp8 = smem + (kb - smem0), *vp8 = smem + (vb - smem0);
             // rows of a score tile: natural keys of the 16, 4-bit: row i is key i ^ (i / 2 % 2) (see the bank note above)
             const int row0 = F4 ? quad ^ ((quad >> 1) & 1) : quad;
-            float sc[SUB][NQ][4];
+            auto key_row = [&](int u, int i) { return (FOLD ? t >> 1 : u) * 16 + row0 + 8 * i; };      // of the tile, of a lane's scores 2 i and 2 i + 1
+            float sc[SC][NQ][4];
+            if constexpr (F4) {
+                float part[SC][NQ][2][4];
 #pragma unroll
-            for (int sub = 0; sub < SUB; ++sub)
-                if constexpr (F4) {
-                    float part[NQ][2][4];
+                for (int sub = 0; sub < SUB; ++sub) {
+                    float sum[NQ][2][4];
 #pragma unroll
                     for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) part[n][0][e] = part[n][1][e] = 0.f;
+                        for (int e = 0; e < 4; ++e) sum[n][0][e] = sum[n][1][e] = 0.f;
                     uint32_t w[2][D / 32];               // 16 (8) bytes of rows row0 and row0 + 8
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -504,22 +532,33 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                         const uint32_t hi[4] = {w0 & 0x00f000f0u, w1 & 0x00f000f0u, u0 & 0x00f000f0u, u1 & 0x00f000f0u};
 #pragma unroll
                         for (int n = 0; n < NQ; ++n) {
-                            mma_f16(part[n][0], lo, qf[n][x][0], qf[n][x][1]);
-                            mma_f16(part[n][1], hi, qf[n][KS / 2 + x][0], qf[n][KS / 2 + x][1]);
+                            mma_f16(sum[n][0], lo, qf[n][x][0], qf[n][x][1]);
+                            mma_f16(sum[n][1], hi, qf[n][KS / 2 + x][0], qf[n][KS / 2 + x][1]);
                         }
                     }
-                    // q.k = sum over the halves of s (q.c) + m sum q
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) part[FOLD ? 0 : sub][n][half][e] = FOLD && sub == 1 && t < 2 ? part[0][n][half][e] : sum[n][half][e];
+                }
+                // q.k = sum over the halves of s (q.c) + m sum q
+#pragma unroll
+                for (int u = 0; u < SC; ++u)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const uint2 pr = *reinterpret_cast<const uint2 *>(vp8 + T * G::kRow + (sub * 16 + row0 + 8 * i) * 8);
+                        const uint2 pr = *reinterpret_cast<const uint2 *>(vp8 + T * G::kRow + key_row(u, i) * 8);
                         const float s0 = __uint_as_float(pr.x << 16), m0 = __uint_as_float(pr.x & 0xffff0000u), s1 = __uint_as_float(pr.y << 16), m1 = __uint_as_float(pr.y & 0xffff0000u);
 #pragma unroll
                         for (int n = 0; n < NQ; ++n)
 #pragma unroll
                             for (int e = 0; e < 2; ++e)
-                                sc[sub][n][2 * i + e] = fmaf(s0, part[n][0][2 * i + e], fmaf(m0, q_sum[n][0][e], fmaf(s1, part[n][1][2 * i + e], m1 * q_sum[n][1][e])));
+                                sc[u][n][2 * i + e] = fmaf(s0, part[u][n][0][2 * i + e], fmaf(m0, q_sum[n][0][e], fmaf(s1, part[u][n][1][2 * i + e], m1 * q_sum[n][1][e])));
                     }
-                } else {
+            } else {
+#pragma unroll
+                for (int sub = 0; sub < SUB; ++sub) {
                     float odd[NQ][4];                    // (two chains of products)
 #pragma unroll
                     for (int n = 0; n < NQ; ++n)
@@ -538,51 +577,52 @@ decode_attn_kernel(const __grid_constant__ Args a) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) sc[sub][n][e] += odd[n][e];
                 }
+            }
             if (stage.x != kAllRows) {
 #pragma unroll
-                for (int sub = 0; sub < SUB; ++sub)
+                for (int u = 0; u < SC; ++u)
 #pragma unroll
                     for (int n = 0; n < NQ; ++n)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (!((stage.x >> (sub * 16 + row0 + 8 * (e >> 1))) & 1)) sc[sub][n][e] = a.scale_log2 < 0.f ? INFINITY : -INFINITY;
+                            if (!((stage.x >> key_row(u, e >> 1)) & 1)) sc[u][n][e] = a.scale_log2 < 0.f ? INFINITY : -INFINITY;
             }
             // Weights against the reference; that moves only where a score would go far above it (and at the first keys): then to the
             // columns' true maxima, the lanes of a column together.
-            float p[SUB][NQ][4];
+            float p[SC][NQ][4];
             bool low = true;
-            uint2 vpar[SUB][2];                  // (4-bit) the values' numbers
+            uint2 vpar[SC][2];                  // (4-bit) the values' numbers
             if constexpr (F4) {
 #pragma unroll
-                for (int sub = 0; sub < SUB; ++sub)
+                for (int u = 0; u < SC; ++u)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        vpar[sub][i] = *reinterpret_cast<const uint2 *>(vp8 + T * (G::kRow + 8) + (sub * 16 + row0 + 8 * i) * 8);
-                        low = low && __uint_as_float(vpar[sub][i].x << 16) * v_unit <= kValueTop && __uint_as_float(vpar[sub][i].y << 16) * v_unit <= kValueTop;
+                        vpar[u][i] = *reinterpret_cast<const uint2 *>(vp8 + T * (G::kRow + 8) + key_row(u, i) * 8);
+                        low = low && __uint_as_float(vpar[u][i].x << 16) <= v_limit && __uint_as_float(vpar[u][i].y << 16) <= v_limit;
                     }
             }
 #pragma unroll
-            for (int sub = 0; sub < SUB; ++sub)
+            for (int u = 0; u < SC; ++u)
 #pragma unroll
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        p[sub][n][e] = fmaf(sc[sub][n][e], unit[n][e & 1], -m[n][e & 1]);
-                        low = low && p[sub][n][e] <= 8.f;
+                        p[u][n][e] = fmaf(sc[u][n][e], unit[n][e & 1], -m[n][e & 1]);
+                        low = low && p[u][n][e] <= 8.f;
                     }
             if (!__all_sync(0xffffffffu, low)) {
                 if constexpr (F4) {              // values far larger than any before: another unit
                     float top = 0.f;
 #pragma unroll
-                    for (int sub = 0; sub < SUB; ++sub)
+                    for (int u = 0; u < SC; ++u)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) top = fmaxf(top, fmaxf(__uint_as_float(vpar[sub][i].x << 16), __uint_as_float(vpar[sub][i].y << 16)));
+                        for (int i = 0; i < 2; ++i) top = fmaxf(top, fmaxf(__uint_as_float(vpar[u][i].x << 16), __uint_as_float(vpar[u][i].y << 16)));
 #pragma unroll
                     for (int o = 1; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    if (top * v_unit > kValueTop && top < INFINITY) {
+                    if (top > v_limit && top < INFINITY) {
                         const float to = __uint_as_float((uint32_t)(127 + 100 + 127 - (int)(__float_as_uint(top) >> 23)) << 23);       // 2^(100 - exponent)
                         const float f = to / v_unit;
-                        v_unit = to;
+                        v_unit = to, v_limit = kValueTop / to;
 #pragma unroll
                         for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -597,7 +637,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                     for (int e = 0; e < 2; ++e) {
                         float top = -INFINITY;
 #pragma unroll
-                        for (int sub = 0; sub < SUB; ++sub) top = fmaxf(top, fmaxf(sc[sub][n][e] * unit[n][e], sc[sub][n][e + 2] * unit[n][e]));
+                        for (int u = 0; u < SC; ++u) top = fmaxf(top, fmaxf(sc[u][n][e] * unit[n][e], sc[u][n][e + 2] * unit[n][e]));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
@@ -609,40 +649,52 @@ decode_attn_kernel(const __grid_constant__ Args a) {
 #pragma unroll
                         for (int d = 0; d < D / 16; ++d) acc[n][d][e] *= f, acc[n][d][e + 2] *= f;
 #pragma unroll
-                        for (int sub = 0; sub < SUB; ++sub)
+                        for (int u = 0; u < SC; ++u)
 #pragma unroll
-                            for (int i = 0; i < 2; ++i) p[sub][n][e + 2 * i] = fmaf(sc[sub][n][e + 2 * i], unit[n][e], -ref);
+                            for (int i = 0; i < 2; ++i) p[u][n][e + 2 * i] = fmaf(sc[u][n][e + 2 * i], unit[n][e], -ref);
                     }
             }
+            uint32_t weight[NQ][2][2];           // (4-bit) the second operand of the values' products, by half and by rows quad and quad + 8
 #pragma unroll
             for (int sub = 0; sub < SUB; ++sub) {
+                if (!FOLD || sub == 0) {
 #pragma unroll
-                for (int n = 0; n < NQ; ++n)
+                    for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        p[sub][n][e] = ex2(p[sub][n][e]);
-                        l[n][e & 1] += p[sub][n][e];
-                    }
+                        for (int e = 0; e < 4; ++e) {
+                            p[FOLD ? 0 : sub][n][e] = ex2(p[FOLD ? 0 : sub][n][e]);
+                            l[n][e & 1] += p[FOLD ? 0 : sub][n][e];
+                        }
+                }
                 if constexpr (F4) {
                     // sum p v = sum (p s) (c - 8) + sum p (m + 8 s), half by half.  p s v_unit is the MMA's operand, rounded to bf16; a code in the
                     // last four bits of a half is the bf16 number c 2^-133 (16 c 2^-133 one nibble higher), a subnormal that needs no
                     // conversion, and -8 of all of them is one more product with the same operand.
-                    uint32_t b[NQ][2][2];
+                    if (!FOLD || sub == 0) {
+                        const int u = FOLD ? 0 : sub;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float vs[2] = {__uint_as_float(vpar[sub][i].x << 16), __uint_as_float(vpar[sub][i].y << 16)};
-                        const float mid[2] = {fmaf(8.f, vs[0], __uint_as_float(vpar[sub][i].x & 0xffff0000u)), fmaf(8.f, vs[1], __uint_as_float(vpar[sub][i].y & 0xffff0000u))};
+                        for (int i = 0; i < 2; ++i) {
+                            const float vs[2] = {__uint_as_float(vpar[u][i].x << 16), __uint_as_float(vpar[u][i].y << 16)};
+                            const float mid[2] = {fmaf(8.f, vs[0], __uint_as_float(vpar[u][i].x & 0xffff0000u)), fmaf(8.f, vs[1], __uint_as_float(vpar[u][i].y & 0xffff0000u))};
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const float su = vs[half] * v_unit;
+                            for (int half = 0; half < 2; ++half) {
+                                const float su = vs[half] * v_unit;
 #pragma unroll
-                            for (int n = 0; n < NQ; ++n) {
-                                b[n][half][i] = transposed(pack_bf16(p[sub][n][2 * i] * su, p[sub][n][2 * i + 1] * su));
+                                for (int n = 0; n < NQ; ++n) {
+                                    weight[n][half][i] = transposed(pack_bf16(p[u][n][2 * i] * su, p[u][n][2 * i + 1] * su));
 #pragma unroll
-                                for (int e = 0; e < 2; ++e) off[n][half][e] = fmaf(p[sub][n][2 * i + e], mid[half], off[n][half][e]);
+                                    for (int e = 0; e < 2; ++e) off[n][half][e] = fmaf(p[u][n][2 * i + e], mid[half], off[n][half][e]);
+                                }
                             }
                         }
                     }
+                    uint32_t b[NQ][2][2];
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) b[n][half][i] = FOLD && quad / 4 != sub ? 0u : weight[n][half][i];
                     // keys of operand rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9, and of each the bytes whose elements this lane's rows of V^T are
                     uint32_t w[4][D / 64];
 #pragma unroll
@@ -849,10 +901,10 @@ constexpr size_t kCounterBytes = 4096;
 size_t workspace_bytes(int sms, int D) { return kCounterBytes + (size_t)sms * 2 * kMaxGroup * (D * sizeof(float) + sizeof(float2)); }
 bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 
-template <int D, bool F4, int NQ>
+template <int D, bool F4, int NQ, bool FOLD = false>
 cudaError_t launch_decode(const Args &a, int sms, cudaStream_t st) {
     using G = Geo<D, F4, NQ>;
-    auto kernel = a.page_size < G::kTile ? decode_attn_kernel<D, F4, NQ, true> : decode_attn_kernel<D, F4, NQ, false>;
+    auto kernel = a.page_size < G::kTile ? decode_attn_kernel<D, F4, NQ, true, FOLD> : decode_attn_kernel<D, F4, NQ, false, FOLD>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kBytes);
     if (e != cudaSuccess) {
         cudaGetLastError();
@@ -883,7 +935,8 @@ int32_t decode_attn(const tessera_model_cfg *cfg, const tessera_decode_desc *d, 
                  static_cast<__nv_bfloat16 *>(out), lse, d->block_table, d->seq_len, d->batch, d->max_pages, d->num_pool_pages, cfg->page_size,
                  cfg->num_q_heads, cfg->num_kv_heads, g, d->window, d->n_sink, scale * 1.4426950408889634f,
                  reinterpret_cast<uint32_t *>(ws), reinterpret_cast<float *>(ws + kCounterBytes), reinterpret_cast<float2 *>(ws + o_ml)};
-    auto launch = D == 128 ? (g <= 8 ? launch_decode<128, F4, 1> : launch_decode<128, F4, 2>) : (g <= 8 ? launch_decode<64, F4, 1> : launch_decode<64, F4, 2>);
+    auto launch = D == 128 ? (F4 && g <= 4 ? launch_decode<128, F4, 1, F4> : g <= 8 ? launch_decode<128, F4, 1> : launch_decode<128, F4, 2>)
+                           : (F4 && g <= 4 ? launch_decode<64, F4, 1, F4> : g <= 8 ? launch_decode<64, F4, 1> : launch_decode<64, F4, 2>);
     const cudaError_t e = launch(a, sms, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return api_set_error(TESSERA_CUDA_ERROR, std::string("decode attention launch: ") + cudaGetErrorName(e) + " (" + cudaGetErrorString(e) + ")");
     return TESSERA_OK;
