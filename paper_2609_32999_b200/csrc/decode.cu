@@ -85,11 +85,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return r;
 }
 // N bytes to shared memory; zeros in place of what is not there.
-template <int N, bool ALL> __device__ __forceinline__ void cp_async(uint32_t dst, const void *src, bool there) {
-    if constexpr (N == 16 && ALL) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-    else if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-    else if constexpr (ALL) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const void *src, bool there) {
+    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(there ? 8 : 0) : "memory");
+}
+template <int N> __device__ __forceinline__ void cp_async(uint32_t dst, const void *src) {
+    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -235,12 +237,21 @@ decode_attn_kernel(const __grid_constant__ Args a) {
             page_ids = i < vis.n && key < vis.len ? a.table[(size_t)r * a.max_pages + (key >> page_shift)] : -1;
         };
         load_pages();
-        // A lane's own places: of its 16 bytes of the rows (and its 8 of their numbers) in page 0 of head 0.
         constexpr int RPT = 32 / CPR;              // rows a turn of 32 lanes
         const uint32_t head_bytes = F4 ? (uint32_t)a.page_size * (D / 2 + 8) : (uint32_t)G::kRow;
         const uint32_t row_bytes = F4 ? (uint32_t)G::kRow : a.H_kv * head_bytes, page_bytes = F4 ? a.H_kv * head_bytes : row_bytes << page_shift;
         const uint32_t numbers = (uint32_t)a.page_size * (D / 2);
+        // A lane's own places: of its 16 bytes of a turn's rows (and its 8 of their numbers) in the keys of page 0, head h, and in a stage.  16-bit
+        // chunks are turned by the row, as ldmatrix wants them; of 4-bit values the halves of rows 4-7 of 8 change places, so that
+        // the four rows and eight columns that a warp's lanes ask for at once lie in different banks.
+        const uint32_t place = lane / CPR * row_bytes + lane % CPR * 16;
+        const uint8_t *lane_k = a.k + (size_t)h * head_bytes + place;
+        const ptrdiff_t to_v = a.v - a.k;
+        const int32_t to_numbers = (int32_t)(numbers + lane * 8) - (int32_t)place;
+        auto chunk_k = [&](int row) { return F4 ? lane % CPR : (lane % CPR) ^ (row & 7); };
+        auto chunk_v = [&](int row) { return F4 && D == 128 ? (lane % CPR) ^ (((row >> 2) & 1) << 1) : chunk_k(row); };
         int run = 0;                               // tiles from j on that are neither first nor last of their pair and all there, pages apart
+        uint32_t plain = 0;                        // stages that hold such a tile
         auto fetch = [&](int at) {
             if (sent < my_tiles) {
                 const int key0 = tile_at(j) * T;
@@ -248,47 +259,48 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                 // the page of row `row` (of any where a page holds the tile)
                 auto page_of = [&](int row) { return __shfl_sync(0xffffffffu, page_ids, SMALL ? (j - jb) * GROUPS + row / 8 : j - jb); };
                 const int page = page_of(lane & (T - 1));
-                uint32_t rows = kAllRows;
-                if (run > 0 && in_pool(page)) {
-                    if (lane == 0) s_stage[warp][at] = make_uint2(kAllRows, 0u);
-                } else {
-                if (SMALL || !(in_pool(page) && key0 + T <= vis.len && (key0 >= vis.first || key0 + T <= vis.sinks))) {
-                    const int key = key0 + (lane & (T - 1));
-                    rows = __ballot_sync(0xffffffffu, key < vis.len && (key < vis.sinks || key >= vis.first) && in_pool(page)) & kAllRows;
-                }
-                if (lane == 0) {
-                    s_stage[warp][at] = make_uint2(rows, (j == 0 ? kFirst : 0u) | (j == vis.n - 1 ? kLast : 0u));
-                    if (j == 0 || sent == 0) s_pair[warp][at] = {r * a.H_kv + h, base + h * vis.n, vis.n};
-                }
-                }
                 const uint32_t kb = ring + at * G::kStageBytes, vb = kb + T * G::kRow;
-                auto copy = [&](auto all_there) {
-                    constexpr bool ALL = decltype(all_there)::value;
-                    // (of a page that is not there nothing is read)
-                    auto page_at = [&](int id) { return (uint64_t)(ALL || in_pool(id) ? (uint32_t)id : 0u) * page_bytes + h * head_bytes; };
-                    const uint64_t p0 = page_at(page) + (key0 & (a.page_size - 1)) * (uint64_t)row_bytes + lane / CPR * row_bytes + lane % CPR * 16;
+                if (!SMALL && run > 0 && in_pool(page)) {
+                    plain |= 1u << at;
+                    const uint8_t *k = lane_k + (uint64_t)(uint32_t)page * page_bytes + (uint64_t)(uint32_t)(key0 & (a.page_size - 1)) * row_bytes;
+                    const uint8_t *v = k + to_v;
 #pragma unroll
                     for (int i = 0; i < T / RPT; ++i) {
-                        const int row = i * RPT + lane / CPR, c = lane % CPR;
-                        uint64_t o = p0 + (uint64_t)(i * RPT) * row_bytes;
-                        if constexpr (SMALL) o = page_at(page_of(row)) + ((key0 + row) & (a.page_size - 1)) * (uint64_t)row_bytes + c * 16;
-                        // 16-bit: chunks turned by the row, as ldmatrix wants them; 4-bit values: the halves of rows 4-7 of 8 change places, so
-                        // that the four rows and eight columns that a warp's lanes ask for at once lie in different banks
-                        const int ck = F4 ? c : c ^ (row & 7), cv = F4 ? (D == 128 ? c ^ (((row >> 2) & 1) << 1) : c) : ck;
-                        cp_async<16, ALL>(kb + row * G::kRow + ck * 16, a.k + o, (rows >> row) & 1);
-                        cp_async<16, ALL>(vb + row * G::kRow + cv * 16, a.v + o, (rows >> row) & 1);
+                        const int row = i * RPT + lane / CPR;
+                        cp_async<16>(kb + row * G::kRow + chunk_k(row) * 16, k + (size_t)(i * RPT) * row_bytes);
+                        cp_async<16>(vb + row * G::kRow + chunk_v(row) * 16, v + (size_t)(i * RPT) * row_bytes);
                     }
-                    if constexpr (F4) {                 // (T = 32: a lane has a row's numbers, and the row's page)
-                        const uint64_t o = page_at(page) + numbers + (SMALL ? (key0 + lane) & (a.page_size - 1) : (key0 & (a.page_size - 1)) + lane) * 8;
-                        cp_async<8, ALL>(vb + T * G::kRow + lane * 8, a.k + o, (rows >> lane) & 1);
-                        cp_async<8, ALL>(vb + T * G::kRow + T * 8 + lane * 8, a.v + o, (rows >> lane) & 1);
+                    if constexpr (F4) {                // (T = 32: a lane has a row's numbers)
+                        // (the rows before the tile's have numbers of 8 bytes where their codes have kRow)
+                        const ptrdiff_t back = to_numbers - (ptrdiff_t)(key0 & (a.page_size - 1)) * (G::kRow - 8);
+                        cp_async<8>(vb + T * G::kRow + lane * 8, k + back);
+                        cp_async<8>(vb + T * G::kRow + T * 8 + lane * 8, v + back);
                     }
-                };
-                if (rows == kAllRows) copy(std::true_type{});
-                else copy(std::false_type{});
+                } else {
+                    plain &= ~(1u << at);
+                    const int mine_row = lane & (T - 1), key = key0 + mine_row;
+                    const uint32_t rows = __ballot_sync(0xffffffffu, key < vis.len && (key < vis.sinks || key >= vis.first) && in_pool(page)) & kAllRows;
+                    if (lane == 0) {
+                        s_stage[warp][at] = make_uint2(rows, (j == 0 ? kFirst : 0u) | (j == vis.n - 1 ? kLast : 0u));
+                        if (j == 0 || sent == 0) s_pair[warp][at] = {r * a.H_kv + h, base + h * vis.n, vis.n};
+                    }
+                    // (of a page that is not there nothing is read)
+                    auto page_at = [&](int id) { return (uint64_t)(in_pool(id) ? (uint32_t)id : 0u) * page_bytes + (uint64_t)h * head_bytes; };
+#pragma unroll
+                    for (int i = 0; i < T / RPT; ++i) {
+                        const int row = i * RPT + lane / CPR;
+                        const uint64_t o = page_at(SMALL ? page_of(row) : page) + (uint64_t)((key0 + row) & (a.page_size - 1)) * row_bytes + lane % CPR * 16;
+                        cp_async<16>(kb + row * G::kRow + chunk_k(row) * 16, a.k + o, (rows >> row) & 1);
+                        cp_async<16>(vb + row * G::kRow + chunk_v(row) * 16, a.v + o, (rows >> row) & 1);
+                    }
+                    if constexpr (F4) {
+                        const uint64_t o = page_at(page) + numbers + (uint64_t)((key0 + lane) & (a.page_size - 1)) * 8;
+                        cp_async<8>(vb + T * G::kRow + lane * 8, a.k + o, (rows >> lane) & 1);
+                        cp_async<8>(vb + T * G::kRow + T * 8 + lane * 8, a.v + o, (rows >> lane) & 1);
+                    }
+                }
                 ++sent, ++j;
-                if (--run > 0) {
-                } else if (sent < my_tiles) {
+                if (--run <= 0 && sent < my_tiles) {
                     if (j == vis.n) {
                         const bool same = jb == 0 && h + 1 < a.H_kv;          // the next head's pages are the ones at hand
                         j = jb = 0;
@@ -299,6 +311,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                                 vis = visible<T>(a.seq_len[++r], a);
                             } while (vis.n == 0);
                         }
+                        lane_k = a.k + (size_t)h * head_bytes + place;
                         if (!same) load_pages();
                     } else if (j - jb == kBatch) {
                         jb = j;
@@ -497,7 +510,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
             cp_wait<G::kStages - 2>();
             __syncwarp();
             fetch(at == 0 ? G::kStages - 1 : at - 1);      // into the stage consumed in the last turn
-            const uint2 stage = s_stage[warp][at];
+            const uint2 stage = (plain >> at) & 1 ? make_uint2(kAllRows, 0u) : s_stage[warp][at];
             if (s == 0 || (stage.y & kFirst)) {
                 now = s_pair[warp][at];
                 begun_here = (stage.y & kFirst) != 0;
