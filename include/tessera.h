@@ -373,7 +373,8 @@ TESSERA_API int32_t tessera_decode_write_kv4(const tessera_model_cfg *cfg, const
  *   q, out: device [batch][H_q][D] bf16, q rotated; lse: device [batch][H_q] fp32, natural log, nullable.
  * A request without a token (or none of whose visible keys has a page in the pool) gets out = 0 and lse = -inf.  Keys on
  * pages outside the pool count as not visible; a length above max_pages * page_size counts as that.  Rows that are not
- * visible are not read.  Results do not depend on the timing of the run.
+ * visible are not read.  Results do not depend on the timing of the run.  Weights of at most 2^8 times values are summed in fp32 and
+ * divided at the end: results are infinite where keys x 2^8 x value reaches 2^128.
  *   workspace: device, tessera_decode_workspace_bytes (a function of head_dim and of the current device), 16-byte aligned.  It must
  *   be all zeros before its first use; every call leaves it ready for the next (captured ones too), and in between it must not be
  *   written.  Calls that may overlap on the GPU - two streams, two graphs - need one each.

@@ -15,7 +15,7 @@
 // before or goes on behind its stretch is a part; at the end the block joins its warps' parts, and parts of pairs that
 // leave the block go to the workspace, where the last block to arrive joins them, always in the order of the tiles.
 // (Blocks that took pairs in turn, all their warps on one, and met at the end of each: 215 us where 64 requests of 200 to
-// 16 384 tokens, 8 heads in 4 bits, take @F4@ us; a join in a kernel of its own: 4 us more for any batch.)
+// 16 384 tokens, 8 heads in 4 bits, take 130 us; a join in a kernel of its own: 4 us more for any batch.)
 // A row that is not visible, past the end or on a page outside the pool is filled with zeros and never read, so what stands
 // there does not matter.
 #include <cmath>
@@ -40,7 +40,7 @@ int32_t api_set_error(int32_t code, const std::string &msg);
 
 namespace {
 
-constexpr float kValueUnit = 18446744073709551616.f;                 // 2^64: products with subnormal codes come out near 2^-69
+constexpr float kValueUnit = 18446744073709551616.f;                 // 2^64: products of subnormal codes with scales near 1 come out near 2^-69
 constexpr float kValueTop = 5192296858534827628530496329220096.f;    // 2^112: p (at most 2^8) times this is a bf16 number
 constexpr int kMaxGroup = 16;
 
@@ -60,7 +60,8 @@ struct Args {
 // Shared memory: every warp's ring (a stage: the rows of a tile of K, of V and, 4-bit, their numbers) and its part of the pair that
 // its stretch begins in; the part of the one it ends in goes into the ring.
 template <int D, bool F4, int NQ> struct Geo {
-    static constexpr int kWarps = F4 && NQ == 1 ? 16 : 8;
+    // (4-bit: 16 warps of 128 registers 135 us, 12 of 168 130, 8 144: 64 requests of up to 16 384 tokens, 8 heads)
+    static constexpr int kWarps = F4 && NQ == 1 ? 12 : 8;
     static constexpr int kThreads = 32 * kWarps;
     static constexpr int kTile = F4 ? 32 : 16;                            // keys
     static constexpr int kRow = F4 ? D / 2 : 2 * D;                       // bytes of a row of K or V
@@ -285,18 +286,21 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                         if (j == 0 || sent == 0) s_pair[warp][at] = {r * a.H_kv + h, base + h * vis.n, vis.n};
                     }
                     // (of a page that is not there nothing is read)
-                    auto page_at = [&](int id) { return (uint64_t)(in_pool(id) ? (uint32_t)id : 0u) * page_bytes + (uint64_t)h * head_bytes; };
+                    auto page_at = [&](int id) { return (uint64_t)(in_pool(id) ? (uint32_t)id : 0u) * page_bytes; };
+                    const int within = key0 & (a.page_size - 1);
+                    const uint8_t *k0 = lane_k + (SMALL ? 0 : page_at(page) + (uint64_t)(uint32_t)within * row_bytes);
 #pragma unroll
                     for (int i = 0; i < T / RPT; ++i) {
                         const int row = i * RPT + lane / CPR;
-                        const uint64_t o = page_at(SMALL ? page_of(row) : page) + (uint64_t)((key0 + row) & (a.page_size - 1)) * row_bytes + lane % CPR * 16;
-                        cp_async<16>(kb + row * G::kRow + chunk_k(row) * 16, a.k + o, (rows >> row) & 1);
-                        cp_async<16>(vb + row * G::kRow + chunk_v(row) * 16, a.v + o, (rows >> row) & 1);
+                        const uint8_t *k = SMALL ? lane_k - place + page_at(page_of(row)) + (uint64_t)((key0 + row) & (a.page_size - 1)) * row_bytes + lane % CPR * 16
+                                                 : k0 + (size_t)(i * RPT) * row_bytes;
+                        cp_async<16>(kb + row * G::kRow + chunk_k(row) * 16, k, (rows >> row) & 1);
+                        cp_async<16>(vb + row * G::kRow + chunk_v(row) * 16, k + to_v, (rows >> row) & 1);
                     }
                     if constexpr (F4) {
-                        const uint64_t o = page_at(page) + numbers + (uint64_t)((key0 + lane) & (a.page_size - 1)) * 8;
-                        cp_async<8>(vb + T * G::kRow + lane * 8, a.k + o, (rows >> lane) & 1);
-                        cp_async<8>(vb + T * G::kRow + T * 8 + lane * 8, a.v + o, (rows >> lane) & 1);
+                        const uint8_t *k = lane_k - place + page_at(page) + numbers + (uint64_t)((key0 + lane) & (a.page_size - 1)) * 8;
+                        cp_async<8>(vb + T * G::kRow + lane * 8, k, (rows >> lane) & 1);
+                        cp_async<8>(vb + T * G::kRow + T * 8 + lane * 8, k + to_v, (rows >> lane) & 1);
                     }
                 }
                 ++sent, ++j;
@@ -624,7 +628,8 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                         low = low && p[u][n][e] <= 8.f;
                     }
             if (!__all_sync(0xffffffffu, low)) {
-                if constexpr (F4) {              // values far larger than any before: another unit
+                if constexpr (F4) {
+                    // The values' unit goes by the first scales of a pair, and changes where far larger ones come.
                     float top = 0.f;
 #pragma unroll
                     for (int u = 0; u < SC; ++u)
@@ -632,9 +637,11 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                         for (int i = 0; i < 2; ++i) top = fmaxf(top, fmaxf(__uint_as_float(vpar[u][i].x << 16), __uint_as_float(vpar[u][i].y << 16)));
 #pragma unroll
                     for (int o = 1; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    if (top > v_limit && top < INFINITY) {
-                        const float to = __uint_as_float((uint32_t)(127 + 100 + 127 - (int)(__float_as_uint(top) >> 23)) << 23);       // 2^(100 - exponent)
-                        const float f = to / v_unit;
+                    const bool begins = __all_sync(0xffffffffu, m[0][0] == -INFINITY);
+                    if ((top > v_limit || (begins && top > 0.f)) && top < INFINITY) {
+                        // 2^(64 - exponent of top), where there is something already 2^(100 - exponent), at most 2^120
+                        const float to = __uint_as_float((uint32_t)min((begins ? 64 : 100) + 254 - (int)(__float_as_uint(top) >> 23), 247) << 23);
+                    const float f = to / v_unit;
                         v_unit = to, v_limit = kValueTop / to;
 #pragma unroll
                         for (int n = 0; n < NQ; ++n)

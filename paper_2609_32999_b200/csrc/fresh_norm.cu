@@ -56,7 +56,7 @@ __device__ __forceinline__ void norm_chunks(float (&lo)[8], float (&hi)[8], cons
 // (cos, sin) of its pairs stay in registers for all heads of its row, and it has kFlight heads' loads in flight.
 constexpr int kRowsPerBlock = 4, kThreadsPerRow = 64, kFlight = 2;
 template <int D, bool INTERLEAVED>
-__global__ void __launch_bounds__(kRowsPerBlock *kThreadsPerRow, 4)
+__global__ void __launch_bounds__(kRowsPerBlock *kThreadsPerRow, 3)
 extend_norm_kernel(Fresh f, uint4 *k_pool, uint4 *v_pool, uint4 *k_cache, uint4 *v_cache, const int32_t *__restrict__ q_pos,
                    const int32_t *__restrict__ fresh_dst, const int32_t *__restrict__ retain_dst, const double *__restrict__ inv_freq,
                    int n_q, int H_q, int H_kv) {
@@ -256,6 +256,7 @@ int32_t check_decode(const tessera_model_cfg *cfg, const tessera_decode_desc *d,
     if (!cfg || !d) return fail(TESSERA_INVALID_ARG, "null cfg or desc");
     const int Hq = cfg->num_q_heads, H = cfg->num_kv_heads, B = cfg->page_size;
     if (Hq <= 0 || H <= 0 || Hq % H != 0) return fail(TESSERA_UNSUPPORTED_SHAPE, "num_q_heads must be a positive multiple of num_kv_heads");
+    if (H > 4096) return fail(TESSERA_UNSUPPORTED_SHAPE, "more than 4 096 KV heads");
     if (Hq / H > 16) return fail(TESSERA_UNSUPPORTED_SHAPE, "group size H_q/H_kv above 16");
     if (cfg->head_dim != 64 && cfg->head_dim != 128) return fail(TESSERA_UNSUPPORTED_SHAPE, "head_dim: only 64 and 128");
     if (B < 8 || B > 128 || (B & (B - 1)) != 0) return fail(TESSERA_UNSUPPORTED_SHAPE, "page_size: a power of two in 8..128");

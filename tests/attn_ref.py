@@ -22,7 +22,7 @@ def attend(q, k, v, pos, window=0, n_sink=0, scale=None, k_size=None, v_size=Non
     s = (torch.einsum("rhd,thd->rht", q, kk) * scale).masked_fill(~seen, -torch.inf)
     ka = kk.abs() if k_size is None else k_size.double().repeat_interleave(g, 1)
     va = vv.abs() if v_size is None else v_size.double().repeat_interleave(g, 1)
-    size = (torch.einsum("rhd,thd->rht", q.abs(), ka) * scale).masked_fill(~seen, 0.0).amax(-1)
+    size = (torch.einsum("rhd,thd->rht", q.abs(), ka) * abs(scale)).masked_fill(~seen, 0.0).amax(-1)
     lse = torch.logsumexp(s, -1)
     w = torch.exp(s - lse[..., None])
     return torch.einsum("rht,thd->rhd", w, vv), lse, torch.einsum("rht,thd->rhd", w, va), size

@@ -121,6 +121,59 @@ def test_score_sizes(q_size, scale, four):
     c.run().check(scale or None)
 
 
+@pytest.mark.parametrize("hq,h,d,page", [(8, 2, 128, 64), (16, 2, 64, 16), (12, 1, 128, 8)])
+@pytest.mark.parametrize("size", [1e-25, 1e-6, 1.0, 1e6, 1e20, 1e33])
+def test_sizes_of_4_bit_values(size, hq, h, d, page):
+    """Values of any size, and a request whose values grow and shrink by far between tiles."""
+    c = Case([1, 90, 700, 40], hq, h, d, page, seed=21, four=True)
+    v = size * torch.randn(c.n_pages, page, h, d, device=DEV)
+    keep = c.v.clone()
+    for r, grow in ((2, [1, 1e-9, 1e4, 1e-3, 1e15]), (3, [1e-6, 1])):
+        for i, f in enumerate(grow):
+            at = torch.from_numpy(c.slots(r)[i * 130:(i + 1) * 130 if i + 1 < len(grow) else None]).to(DEV)
+            v.view(-1, h, d)[at] *= min(f, 1e37 / size / 16)
+    new, page_of = k4.pool4(v.to(torch.bfloat16)), torch.from_numpy(np.concatenate([c.slots(r) for r in range(4)])).to(DEV)
+    split = lambda x: (x[:, :, : page * (d // 2)].view(c.n_pages, h, page, d // 2), x[:, :, page * (d // 2):].view(c.n_pages, h, page, 8))
+    for a, b in zip(split(keep), split(new)):
+        a[page_of // page, :, page_of % page] = b[page_of // page, :, page_of % page]
+    c.v.copy_(keep)
+    c.run().check()
+
+
+def test_4_bit_rows_of_one_value_and_of_nan():
+    c = Case([200, 77, 64], 8, 2, 128, 16, seed=22, four=True)
+    d, page = 128, 16
+    par = c.v[:, :, page * (d // 2):].view(c.n_pages, 2, page, 8)
+    at = torch.from_numpy(c.slots(0)).to(DEV)
+    par[at // page, :, at % page] = torch.tensor([0, 0, 0x80, 0x7E, 0, 0, 0x80, 0xBF], dtype=torch.uint8, device=DEV)      # scales 0, leasts 2^126 and -1
+    par = c.k[:, :, page * (d // 2):].view(c.n_pages, 2, page, 8)
+    bad = int(c.slots(1)[50])
+    par[bad // page, 1, bad % page] = torch.tensor([0xC0, 0x7F] * 4, dtype=torch.uint8, device=DEV)
+    c.run()
+    torch.cuda.synchronize()
+    # weights of 200 equal values sum to far more than 4 before they are divided by: 4 times 2^126 is no fp32 number any more
+    assert c.out[0, :, :64].isinf().all() and (c.out[0, :, 64:] == -1).all()
+    par = c.v[:, :, page * (d // 2):].view(c.n_pages, 2, page, 8)
+    par[at // page, :, at % page] = torch.tensor([0, 0, 0x80, 0x71, 0, 0, 0x80, 0xBF], dtype=torch.uint8, device=DEV)      # 2^100
+    c.run()
+    assert (c.out[0, :, :64].float() == 2.0 ** 100).all() and (c.out[0, :, 64:] == -1).all()
+    assert c.out[1, 4:].isnan().all() and c.lse[1, 4:].isnan().all() and c.out[1, :4].isfinite().all() and c.lse[1, :4].isfinite().all()
+    assert c.out[2].isfinite().all()
+
+
+@pytest.mark.parametrize("q_size", [1e-30, 1e-4, 1e4])
+def test_sizes_of_queries_over_4_bit_keys(q_size):
+    c = Case([1, 90, 700], 8, 2, 128, 64, seed=23, four=True, q_size=q_size, scale=0.088 / q_size if q_size > 1 else 0.0)
+    c.q[1, 3, 5:] = 0
+    c.q[2, 2] *= 2.0 ** torch.linspace(-40, 0, 128, device=DEV)
+    c.run().check(0.088 / q_size if q_size > 1 else None)
+
+
+@pytest.mark.parametrize("four", [False, True])
+def test_negative_scale(four):
+    Case([1, 33, 1000], 8, 2, 128, 64, seed=24, four=four, scale=-0.3, window=300, n_sink=5).run().check(-0.3)
+
+
 @pytest.mark.parametrize("four", [False, True])
 def test_pages_outside_the_pool_and_lengths_past_the_table(four):
     c = Case([300, 130, 64, 200], 8, 2, 128, 16, seed=4, four=four, wide=0)
