@@ -66,13 +66,13 @@ template <int D, bool F4, int NQ> struct Geo {
     static constexpr int kTile = F4 ? 32 : 16;                            // keys
     static constexpr int kRow = F4 ? D / 2 : 2 * D;                       // bytes of a row of K or V
     static constexpr int kStageBytes = 2 * kTile * (kRow + (F4 ? 8 : 0));
+    static constexpr int kFew = F4 ? 44 : 56;                             // tiles that a block may have more for whole pairs (see stretch_of)
     static constexpr int kPart = 8 * NQ * (D + 4);                        // floats; rows 4 apart in banks: the lanes of a store spread over all
     static constexpr int kStages = F4 ? (NQ == 1 ? 2 : 4) * (128 / D) : (NQ == 1 ? 3 : 2) * (128 / D);
     static constexpr int kRing = kWarps * kStages * kStageBytes;
     static constexpr int kBytes = kRing + kWarps * kPart * 4;
-    static constexpr int kChainBytes = (kWarps + 1) * 8 * NQ * 8;         // of the join, behind the part in the first warp's ring
     static_assert(kTile % kDecodeUnit == 0, "");
-    static_assert(kStages * kStageBytes >= kPart * 4 + kChainBytes, "a part goes into a warp's ring");
+    static_assert(kStages * kStageBytes >= kPart * 4, "a part goes into a warp's ring");
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -150,34 +150,75 @@ __device__ __forceinline__ int worker_of(int x, int workers, int all) {
 
 // A warp's stretch of the batch's `all` tiles: [first, last), beginning in request r, before which lie `before` tiles.  Every warp sums the
 // batch by itself, a stretch of the requests a lane: no waiting for others, and the lengths are in L1 after the first.
+// As a rule all warps of the grid, `workers` of them, share the tiles evenly.  Where that makes no block's share much larger, blocks
+// share the pairs instead, whole, and a block's warps their tiles: no parts leave a block then, and joining them takes 3 to 5 us.
+// "Much": by more than `few` tiles, by the bound pairs a block x tiles of the longest pair.  (One request of 300 tokens, 8 heads, 9.1 ->
+// 6.0 us, 4-bit 10.9 -> 6.7; 16 of 900 14.3 -> 10.3; alone 1 300 tokens would take 11.5 for 9.8.)
 struct Stretch { int first, last, all, workers, r, before; };
-template <int T>
-__device__ __forceinline__ Stretch stretch_of(const Args &a, int worker, int most) {
-    const int lane = threadIdx.x & 31, per = (a.batch + 31) / 32, r0 = lane * per, r1 = min(a.batch, r0 + per);
-    auto tiles = [&](int r) { return a.H_kv * visible<T>(a.seq_len[r], a).n; };
-    int own = 0;
-    for (int r = r0; r < r1; ++r) own += tiles(r);
-    int end = own;
+template <int T, int NW>
+__device__ __forceinline__ Stretch stretch_of(const Args &a, int few) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, per = (a.batch + 31) / 32, r0 = lane * per, r1 = min(a.batch, r0 + per);
+    auto tiles = [&](int r) { return visible<T>(a.seq_len[r], a).n; };
+    int own = 0, some = 0, most = 0;                  // tiles, requests that have any, tiles of a head of the longest
+    for (int r = r0; r < r1; ++r) {
+        const int n = tiles(r);
+        own += n * a.H_kv, some += n > 0, most = max(most, n);
+    }
+    int end = own, count = some;
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
-        const int y = __shfl_up_sync(0xffffffffu, end, o);
-        if (lane >= o) end += y;
+        const int x = __shfl_up_sync(0xffffffffu, end, o), y = __shfl_up_sync(0xffffffffu, count, o);
+        if (lane >= o) end += x, count += y;
     }
+    most = __reduce_max_sync(0xffffffffu, most);
+    // The request that has the x-th tile, respectively the x-th that has any, and the tiles before it: the lane whose stretch it is in walks.
+    auto find = [&](int x, bool by_tile, int &r, int &before) {
+        int passed = by_tile ? end - own : count - some;
+        const bool mine = passed <= x && x < (by_tile ? end : count);
+        r = r0, before = end - own;
+        if (mine)
+            for (;; ++r) {
+                const int n = tiles(r) * a.H_kv, step = by_tile ? n : n > 0;
+                if (x < passed + step) break;
+                passed += step, before += n;
+            }
+        const int src = __ffs(__ballot_sync(0xffffffffu, mine)) - 1;
+        r = __shfl_sync(0xffffffffu, r, src);
+        before = __shfl_sync(0xffffffffu, before, src);
+    };
     Stretch s;
     s.all = __shfl_sync(0xffffffffu, end, 31);
-    s.workers = min(most, s.all);
+    const int grid = (int)gridDim.x, pairs = __shfl_sync(0xffffffffu, count, 31) * a.H_kv;
+    const bool whole = (int64_t)((pairs + grid - 1) / grid) * most <= few + s.all / grid;
+    s.workers = min(grid * NW, s.all);
     s.first = s.last = s.all;
     s.r = s.before = 0;
-    if (worker >= s.workers) return s;                // (where there are fewer tiles than warps the first warps have one each)
-    s.first = first_tile(worker, s.workers, s.all);
-    s.last = first_tile(worker + 1, s.workers, s.all);
-    const bool mine = end - own <= s.first && s.first < end;
-    int r = r0, before = end - own;
-    if (mine)
-        for (int n = tiles(r); before + n <= s.first; n = tiles(r)) before += n, ++r;
-    const int from = __ffs(__ballot_sync(0xffffffffu, mine)) - 1;
-    s.r = __shfl_sync(0xffffffffu, r, from);
-    s.before = __shfl_sync(0xffffffffu, before, from);
+    const int blocks = min(grid, pairs);
+    if (whole ? (int)blockIdx.x >= blocks : (int)blockIdx.x * NW + warp >= s.workers) return s;       // (fewer tiles than warps: the first have one each)
+    if (whole) {
+        int first, last;
+        if (pairs <= grid) {                           // a pair each
+            find((int)blockIdx.x / a.H_kv, false, s.r, s.before);
+            const int n = tiles(s.r);
+            first = s.before + (int)blockIdx.x % a.H_kv * n, last = first + n;
+        } else {
+            auto first_of = [&](int pair) {            // the pair's first tile
+                if (pair == pairs) return s.all;
+                int r, before;
+                find(pair / a.H_kv, false, r, before);
+                return before + pair % a.H_kv * tiles(r);
+            };
+            first = first_of(first_tile(blockIdx.x, blocks, pairs)), last = first_of(first_tile(blockIdx.x + 1, blocks, pairs));
+        }
+        const int mates = min(NW, last - first);
+        s.first = warp < mates ? first + first_tile(warp, mates, last - first) : last;
+        s.last = warp < mates ? first + first_tile(warp + 1, mates, last - first) : last;
+        if (warp >= mates || pairs <= grid) return s;
+    } else {
+        s.first = first_tile((int)blockIdx.x * NW + warp, s.workers, s.all);
+        s.last = first_tile((int)blockIdx.x * NW + warp + 1, s.workers, s.all);
+    }
+    find(s.first, true, s.r, s.before);
     return s;
 }
 
@@ -208,14 +249,14 @@ decode_attn_kernel(const __grid_constant__ Args a) {
     __shared__ Pair s_pair[NW][G::kStages];           // of a stage that is its pair's first, or the warp's
     __shared__ float2 s_ml[NW][2][Q8];
     __shared__ Pair s_part[NW][2];                    // [0]: of a pair that began before the warp's stretch, [1]: of one that goes on behind it
-    __shared__ int s_first[NW + 1], s_length[NW + 1], s_leaves[2], s_join[2][2];
+    __shared__ int s_first[NW + 1], s_leaves[2], s_join[2][2];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, quad = lane / 4, t = lane % 4;
     const int page_shift = __ffs(a.page_size) - 1;
     if (lane < 2) s_part[warp][lane] = {0, 0, -1};
     if (tid < 2) s_leaves[tid] = -1;
     grid_wait();
     grid_release();
-    const Stretch mine = stretch_of<T>(a, (int)blockIdx.x * NW + warp, (int)gridDim.x * NW);
+    const Stretch mine = stretch_of<T, NW>(a, G::kFew);
     if (lane == 0) {
         s_first[warp] = mine.first;
         if (warp == NW - 1) s_first[NW] = mine.last;
@@ -261,8 +302,19 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                 auto page_of = [&](int row) { return __shfl_sync(0xffffffffu, page_ids, SMALL ? (j - jb) * GROUPS + row / 8 : j - jb); };
                 const int page = page_of(lane & (T - 1));
                 const uint32_t kb = ring + at * G::kStageBytes, vb = kb + T * G::kRow;
+                uint32_t rows = kAllRows;
                 if (!SMALL && run > 0 && in_pool(page)) {
                     plain |= 1u << at;
+                } else {
+                    plain &= ~(1u << at);
+                    const int key = key0 + (lane & (T - 1));
+                    rows = __ballot_sync(0xffffffffu, key < vis.len && (key < vis.sinks || key >= vis.first) && in_pool(page)) & kAllRows;
+                    if (lane == 0) {
+                        s_stage[warp][at] = make_uint2(rows, (j == 0 ? kFirst : 0u) | (j == vis.n - 1 ? kLast : 0u));
+                        if (j == 0 || sent == 0) s_pair[warp][at] = {r * a.H_kv + h, base + h * vis.n, vis.n};
+                    }
+                }
+                if (!SMALL && rows == kAllRows) {
                     const uint8_t *k = lane_k + (uint64_t)(uint32_t)page * page_bytes + (uint64_t)(uint32_t)(key0 & (a.page_size - 1)) * row_bytes;
                     const uint8_t *v = k + to_v;
 #pragma unroll
@@ -278,13 +330,6 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                         cp_async<8>(vb + T * G::kRow + T * 8 + lane * 8, v + back);
                     }
                 } else {
-                    plain &= ~(1u << at);
-                    const int mine_row = lane & (T - 1), key = key0 + mine_row;
-                    const uint32_t rows = __ballot_sync(0xffffffffu, key < vis.len && (key < vis.sinks || key >= vis.first) && in_pool(page)) & kAllRows;
-                    if (lane == 0) {
-                        s_stage[warp][at] = make_uint2(rows, (j == 0 ? kFirst : 0u) | (j == vis.n - 1 ? kLast : 0u));
-                        if (j == 0 || sent == 0) s_pair[warp][at] = {r * a.H_kv + h, base + h * vis.n, vis.n};
-                    }
                     // (of a page that is not there nothing is read)
                     auto page_at = [&](int id) { return (uint64_t)(in_pool(id) ? (uint32_t)id : 0u) * page_bytes; };
                     const int within = key0 & (a.page_size - 1);
@@ -778,79 +823,51 @@ decode_attn_kernel(const __grid_constant__ Args a) {
     // ---- the block's parts.  A chain is one pair's: a part at a stretch's end (c - 1 is the warp; or, c = 0, of a pair that began before
     // the block, at the first stretch's beginning), then the following warps' parts at their beginnings.
     const int first = s_first[0], last = s_first[NW];      // the block's tiles
-    float2 *s_chain = reinterpret_cast<float2 *>(smem + G::kPart * 4);        // [NW + 1][Q8] reference and sum of a chain
-    for (int i = tid; i < (NW + 1) * Q8; i += NT) {
-        const int c = i / Q8, col = i % Q8, w0 = max(c - 1, 0), which = c == 0 ? 0 : 1;
+    for (uint32_t left = __ballot_sync(0xffffffffu, lane <= NW && s_part[max(min(lane, NW) - 1, 0)][lane == 0 ? 0 : 1].tiles >= 0); left; left &= left - 1) {
+        const int c = __ffs(left) - 1, w0 = max(c - 1, 0), which = c == 0 ? 0 : 1;
         const Pair pt = s_part[w0][which];
-        int n = 0;                                          // warps with a part of it
-        if (pt.tiles >= 0) {
-            const int end = pt.begin + pt.tiles;
-            n = 1;
-            float2 ml[NW];                                  // (all loads at once)
-#pragma unroll
-            for (int w = 1; w < NW; ++w) n += w > w0 && s_first[w] < end;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) ml[w] = s_ml[min(w0 + w, NW - 1)][w ? 0 : which][col];
-            float top = ml[0].x;
-#pragma unroll
-            for (int w = 1; w < NW; ++w) top = w < n ? fmaxf(top, ml[w].x) : top;
-            const float ref = top == -INFINITY ? 0.f : top;
-            float sum = 0.f;
-#pragma unroll
-            for (int w = 0; w < NW; ++w)
-                if (w < n) {
-                    const float f = ex2(ml[w].x - ref);
-                    s_ml[w0 + w][w ? 0 : which][col].x = f;              // the part's weight from here on
-                    sum = fmaf(ml[w].y, f, sum);
-                }
-            s_chain[c * Q8 + col] = make_float2(top, sum);
-            if (col == 0 && !(pt.begin >= first && end <= last)) s_leaves[pt.begin >= first ? 1 : 0] = c;
-        }
-        if (col == 0) s_length[c] = n;
-    }
-    __syncthreads();
-    for (uint32_t left = __ballot_sync(0xffffffffu, lane <= NW && s_length[min(lane, NW)] > 0); left; left &= left - 1) {
-        const int c = __ffs(left) - 1, n = s_length[c];
-        const int w0 = max(c - 1, 0), which = c == 0 ? 0 : 1;
-        const Pair pt = s_part[w0][which];
-        const bool here = pt.begin >= first && pt.begin + pt.tiles <= last;
+        const int end = pt.begin + pt.tiles;
+        const int n = 1 + __popc(__ballot_sync(0xffffffffu, lane > w0 && lane < NW && s_first[min(lane, NW)] < end));        // warps with a part of it
+        const bool here = pt.begin >= first && end <= last;
+        if (tid == 0 && !here) s_leaves[pt.begin >= first ? 1 : 0] = c;
         const size_t slot = 2 * (size_t)blockIdx.x + (pt.begin >= first ? 1 : 0);
         const size_t head0 = (size_t)(pt.pair / a.H_kv) * a.H_q + pt.pair % a.H_kv * a.g;
         for (int i = tid; i < a.g * (D / 2); i += NT) {
             const int col = i / (D / 2), el = i % (D / 2) * 2;
             const float *src0 = which == 1 ? reinterpret_cast<const float *>(smem + w0 * G::kStages * G::kStageBytes)
                                            : reinterpret_cast<const float *>(smem + G::kRing) + w0 * G::kPart;
+            float2 ml[NW];                                  // (all loads at once)
+#pragma unroll
+            for (int w = 0; w < NW; ++w) ml[w] = w < n ? s_ml[min(w0 + w, NW - 1)][w ? 0 : which][col] : make_float2(-INFINITY, 0.f);
+            float top = ml[0].x;
+#pragma unroll
+            for (int w = 1; w < NW; ++w) top = fmaxf(top, ml[w].x);
+            const float ref = top == -INFINITY ? 0.f : top;
             float2 o = *reinterpret_cast<const float2 *>(src0 + col * RP + el);
-            const float f0 = s_ml[w0][which][col].x;
-            o.x *= f0, o.y *= f0;
-            for (int w1 = 1; w1 < n; w1 += 4) {
-                float2 y[4];
-                float f[4];
+            float f = ex2(ml[0].x - ref), sum = ml[0].y * f;
+            o.x *= f, o.y *= f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int w = min(w0 + w1 + i, NW - 1);
-                    y[i] = *reinterpret_cast<const float2 *>(reinterpret_cast<const float *>(smem + G::kRing) + w * G::kPart + col * RP + el);
-                    f[i] = s_ml[w][0][col].x;
+            for (int w = 1; w < NW; ++w)
+                if (w < n) {
+                    const float2 y = *reinterpret_cast<const float2 *>(reinterpret_cast<const float *>(smem + G::kRing) + (w0 + w) * G::kPart + col * RP + el);
+                    f = ex2(ml[w].x - ref);
+                    sum = fmaf(ml[w].y, f, sum);
+                    o.x = fmaf(y.x, f, o.x), o.y = fmaf(y.y, f, o.y);
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (w1 + i < n) o.x = fmaf(y[i].x, f[i], o.x), o.y = fmaf(y[i].y, f[i], o.y);
-            }
-            const float2 all = s_chain[c * Q8 + col];
             if (here) {
-                const float inv = all.x == -INFINITY ? 0.f : 1.f / all.y;
+                const float inv = top == -INFINITY ? 0.f : 1.f / sum;
                 *reinterpret_cast<uint32_t *>(a.out + (head0 + col) * D + el) = pack_bf16(o.x * inv, o.y * inv);
-                if (a.lse && el == 0) a.lse[head0 + col] = all.x == -INFINITY ? -INFINITY : (all.x + log2f(all.y)) * 0.6931471805599453f;
+                if (a.lse && el == 0) a.lse[head0 + col] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
             } else {
                 __stcg(reinterpret_cast<float2 *>(a.ws_o + (slot * kMaxGroup + col) * D + el), o);
-                if (el == 0) __stcg(a.ws_ml + slot * kMaxGroup + col, all);
+                if (el == 0) __stcg(a.ws_ml + slot * kMaxGroup + col, make_float2(top, sum));
             }
         }
     }
+    __syncthreads();
     // A pair that leaves the block (two at most: one that began before it, one that goes on behind it) has parts with the blocks b0 .. b1;
     // the last of them to arrive joins them, in their order.
     if (s_leaves[0] < 0 && s_leaves[1] < 0) return empty_requests<D, NT, T>(a);
-    __syncthreads();
     if (tid < 64 && lane == 0 && s_leaves[warp] >= 0) {
         const int c = s_leaves[warp];
         const Pair pt = s_part[max(c - 1, 0)][c == 0 ? 0 : 1];
