@@ -249,7 +249,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
     __shared__ Pair s_pair[NW][G::kStages];           // of a stage that is its pair's first, or the warp's
     __shared__ float2 s_ml[NW][2][Q8];
     __shared__ Pair s_part[NW][2];                    // [0]: of a pair that began before the warp's stretch, [1]: of one that goes on behind it
-    __shared__ int s_first[NW + 1], s_leaves[2], s_join[2][2];
+    __shared__ int s_first[NW + 1], s_leaves[2], s_join[2][2], s_shared[2];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, quad = lane / 4, t = lane % 4;
     const int page_shift = __ffs(a.page_size) - 1;
     if (lane < 2) s_part[warp][lane] = {0, 0, -1};
@@ -257,8 +257,9 @@ decode_attn_kernel(const __grid_constant__ Args a) {
     grid_wait();
     grid_release();
     const Stretch mine = stretch_of<T, NW>(a, G::kFew);
-    if (lane == 0) {
+    if (lane == 0) {                                  // (kept for the end)
         s_first[warp] = mine.first;
+        s_shared[0] = mine.workers, s_shared[1] = mine.all;
         if (warp == NW - 1) s_first[NW] = mine.last;
     }
     const int my_tiles = mine.last - mine.first;
@@ -871,7 +872,8 @@ decode_attn_kernel(const __grid_constant__ Args a) {
     if (tid < 64 && lane == 0 && s_leaves[warp] >= 0) {
         const int c = s_leaves[warp];
         const Pair pt = s_part[max(c - 1, 0)][c == 0 ? 0 : 1];
-        const int b0 = worker_of(pt.begin, mine.workers, mine.all) / NW, b1 = worker_of(pt.begin + pt.tiles - 1, mine.workers, mine.all) / NW;
+        const int workers = s_shared[0], all = s_shared[1];
+        const int b0 = worker_of(pt.begin, workers, all) / NW, b1 = worker_of(pt.begin + pt.tiles - 1, workers, all) / NW;
         uint32_t before;                               // (back to 0 with the last)
         asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(before) : "l"(a.ws_count + b0), "r"((uint32_t)(b1 - b0)) : "memory");
         s_join[warp][0] = b0;
