@@ -99,12 +99,11 @@ _lib.tessera_rope_shift_static.argtypes = [ctypes.POINTER(ModelCfg), _vp, ctypes
                                            _I32P, ctypes.c_int32, _vp]
 _lib.tessera_selftest_bounded_wait.argtypes = [ctypes.c_int64, _I32P, ctypes.POINTER(ctypes.c_int64), _vp]
 _lib.tessera_kv_retain_kv4.argtypes = _lib.tessera_kv_compose_from_kv4.argtypes = [_vp, _vp, _vp, _vp, _vp, ctypes.c_uint32, _vp]
-_lib.tessera_extend_write_norm.argtypes = [_vp, _vp, _vp, ctypes.POINTER(FreshRows), _vp, _vp, _vp]
-_lib.tessera_decode_write.argtypes = _lib.tessera_decode_write_kv4.argtypes = [ctypes.POINTER(ModelCfg), ctypes.POINTER(DecodeDesc), _vp, _vp,
-                                                                               ctypes.POINTER(FreshRows), _vp]
-_lib.tessera_decode_workspace_bytes.argtypes = [ctypes.POINTER(ModelCfg), ctypes.POINTER(ctypes.c_int64)]
-_lib.tessera_decode_attn.argtypes = _lib.tessera_decode_attn_kv4.argtypes = [ctypes.POINTER(ModelCfg), ctypes.POINTER(DecodeDesc), _vp, _vp, _vp, _vp,
-                                                                             _vp, _vp, ctypes.c_int64, _vp]
+# (structures by address: ctypes takes an integer in half the time it takes to check a typed pointer)
+_lib.tessera_extend_write_norm.argtypes = [_vp] * 7
+_lib.tessera_decode_write.argtypes = _lib.tessera_decode_write_kv4.argtypes = [_vp] * 6
+_lib.tessera_decode_workspace_bytes.argtypes = [_vp, ctypes.POINTER(ctypes.c_int64)]
+_lib.tessera_decode_attn.argtypes = _lib.tessera_decode_attn_kv4.argtypes = [_vp] * 8 + [ctypes.c_int64, _vp]
 _lib.tessera_last_error.argtypes = [ctypes.c_char_p, ctypes.c_int32]
 _lib.tessera_launch_count.argtypes = []
 _lib.tessera_launch_count.restype = ctypes.c_int64
@@ -161,31 +160,31 @@ def _model_cfg(sh, inv: Optional[np.ndarray]) -> ModelCfg:
                     int(sh.rope_pairing), float(sh.sm_scale))
 
 
-def _expect(what: str, t, index: int, dtype, shape, rows: bool = False) -> None:
-    """Device, type and shape of a tensor; contiguous, or (rows) with heads side by side inside rows any distance apart."""
+def _expect(what: str, t, index: int, dtype, shape, rows: bool = False) -> int:
+    """Device, type and shape of a tensor; contiguous, or (rows) with heads side by side inside rows any distance apart: returned in
+    elements, 0 where the tensor is contiguous."""
     if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
-        return
+        return 0
     if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
         raise ValueError("%s: expected %s of %s on device %d, got %s of %s on device %d"
                          % (what, tuple(shape), dtype, index, tuple(t.shape), t.dtype, t.get_device()))
     if not (rows and t.stride()[1:] == (shape[2], 1) and t.stride(0) >= shape[1] * shape[2]):
         raise ValueError("%s: strides %s" % (what, tuple(t.stride())))
+    return t.stride(0)
 
 
 def _fresh_rows(sh, n: int, index: int, bfloat16, q, q_out, k, v, q_weight, k_weight, eps) -> FreshRows:
     hq, h, d = sh.num_q_heads, sh.num_kv_heads, sh.head_dim
+    q_row = 0
     if q is not None:
-        _expect("q", q, index, bfloat16, (n, hq, d), rows=True)
+        q_row = _expect("q", q, index, bfloat16, (n, hq, d), rows=True)
         _expect("q_out", q_out, index, bfloat16, (n, hq, d))
-    _expect("k_new", k, index, bfloat16, (n, h, d), rows=True)
-    _expect("v_new", v, index, bfloat16, (n, h, d), rows=True)
+    k_row, v_row = _expect("k_new", k, index, bfloat16, (n, h, d), rows=True), _expect("v_new", v, index, bfloat16, (n, h, d), rows=True)
     if q_weight is not None:
         _expect("q_weight", q_weight, index, bfloat16, (d,))
     if k_weight is not None:
         _expect("k_weight", k_weight, index, bfloat16, (d,))
-    one = n < 2                            # (the stride of a single row means nothing)
-    return FreshRows(_dev(q), k.data_ptr(), v.data_ptr(), None if q is None else q_out.data_ptr(), 0 if one or q is None else q.stride(0),
-                     0 if one else k.stride(0), 0 if one else v.stride(0), _dev(q_weight), _dev(k_weight), eps)
+    return FreshRows(_dev(q), k.data_ptr(), v.data_ptr(), None if q is None else q_out.data_ptr(), q_row, k_row, v_row, _dev(q_weight), _dev(k_weight), eps)
 
 
 class Plan:
@@ -292,7 +291,7 @@ class Plan:
         v_new may be slices [n_q, heads, D] of a fused projection.  q None: keys and values alone."""
         from torch import bfloat16
         rows = _fresh_rows(self.shape, int(self.info.n_q), k_new_raw.get_device(), bfloat16, q, q_out, k_new_raw, v_new, q_weight, k_weight, eps)
-        _check(_lib.tessera_extend_write_norm(self._h, _dev(k_pool), _dev(v_pool), ctypes.byref(rows), _dev(k_cache), _dev(v_cache), _stream(stream)))
+        _check(_lib.tessera_extend_write_norm(self._h, _dev(k_pool), _dev(v_pool), ctypes.addressof(rows), _dev(k_cache), _dev(v_cache), _stream(stream)))
 
     def partial_prefill_attn(self, k_pool, v_pool, q, k_new, v_new, out, lse=None, stream=None) -> None:
         _check(_lib.tessera_partial_prefill_attn(self._h, _dev(k_pool), _dev(v_pool), _dev(q), _dev(k_new),
@@ -368,7 +367,7 @@ class Decode:
         self._cfg = _model_cfg(shape, self._inv)
         self.block_table, self.seq_lens, self.num_pool_pages = block_table, seq_lens, int(num_pool_pages)
         self._desc = DecodeDesc(self.batch, int(block_table.shape[1]), _dev(block_table), _dev(seq_lens), self.num_pool_pages, int(window), int(n_sink))
-        self._args = ctypes.byref(self._cfg), ctypes.byref(self._desc)
+        self._args = ctypes.addressof(self._cfg), ctypes.addressof(self._desc)
         need = ctypes.c_int64(0)
         with torch.cuda.device(self.device):
             _check(_lib.tessera_decode_workspace_bytes(self._args[0], ctypes.byref(need)))
@@ -388,7 +387,7 @@ class Decode:
 
     def _write(self, call, k_pool, v_pool, q, q_out, k_new, v_new, q_weight, k_weight, eps, stream) -> None:
         rows = _fresh_rows(self.shape, self.batch, self._index, self._bf16, q, q_out, k_new, v_new, q_weight, k_weight, eps)
-        _check(call(*self._args, k_pool.data_ptr(), v_pool.data_ptr(), ctypes.byref(rows), stream))
+        _check(call(*self._args, k_pool.data_ptr(), v_pool.data_ptr(), ctypes.addressof(rows), stream))
 
     def write(self, k_pool, v_pool, q, q_out, k_new, v_new, q_weight=None, k_weight=None, eps: float = 1e-6, stream=None) -> None:
         """The new tokens' un-rotated rows: q (normalised with q_weight, rotated) to q_out, k (likewise) and v to their slots.  q, k_new and v_new

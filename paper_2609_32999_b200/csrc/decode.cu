@@ -989,23 +989,25 @@ using namespace tessera;
 extern "C" {
 
 int32_t tessera_decode_workspace_bytes(const tessera_model_cfg *cfg, int64_t *bytes) {
-    if (!cfg || !bytes) return api_set_error(TESSERA_INVALID_ARG, "null cfg or bytes");
-    *bytes = 0;
-    if (cfg->head_dim != 64 && cfg->head_dim != 128) return api_set_error(TESSERA_UNSUPPORTED_SHAPE, "head_dim: only 64 and 128");
-    const int sms = sm_count();
-    if (sms <= 0) return api_set_error(TESSERA_CUDA_ERROR, "no current device");
-    *bytes = (int64_t)workspace_bytes(sms, cfg->head_dim);
-    return TESSERA_OK;
+    return guarded([&]() -> int32_t {
+        if (!cfg || !bytes) return api_set_error(TESSERA_INVALID_ARG, "null cfg or bytes");
+        *bytes = 0;
+        if (cfg->head_dim != 64 && cfg->head_dim != 128) return api_set_error(TESSERA_UNSUPPORTED_SHAPE, "head_dim: only 64 and 128");
+        const int sms = sm_count();
+        if (sms <= 0) return api_set_error(TESSERA_CUDA_ERROR, "no current device");
+        *bytes = (int64_t)workspace_bytes(sms, cfg->head_dim);
+        return TESSERA_OK;
+    });
 }
 
 int32_t tessera_decode_attn(const tessera_model_cfg *cfg, const tessera_decode_desc *desc, const void *k_pool, const void *v_pool, const void *q,
                             void *out, float *lse, void *workspace, int64_t workspace_bytes, void *stream) {
-    return decode_attn<false>(cfg, desc, k_pool, v_pool, q, out, lse, workspace, workspace_bytes, stream);
+    return guarded([&] { return decode_attn<false>(cfg, desc, k_pool, v_pool, q, out, lse, workspace, workspace_bytes, stream); });
 }
 
 int32_t tessera_decode_attn_kv4(const tessera_model_cfg *cfg, const tessera_decode_desc *desc, const void *k_pool4, const void *v_pool4, const void *q,
                                 void *out, float *lse, void *workspace, int64_t workspace_bytes, void *stream) {
-    return decode_attn<true>(cfg, desc, k_pool4, v_pool4, q, out, lse, workspace, workspace_bytes, stream);
+    return guarded([&] { return decode_attn<true>(cfg, desc, k_pool4, v_pool4, q, out, lse, workspace, workspace_bytes, stream); });
 }
 
 }  // extern "C"

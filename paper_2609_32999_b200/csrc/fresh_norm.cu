@@ -249,6 +249,31 @@ int32_t decode_write(const tessera_model_cfg *cfg, const tessera_decode_desc *d,
     return launched(launch_grid(kernel, grid, kStepThreads, 0, static_cast<cudaStream_t>(stream), true, f, k_pool, v_pool, s), "launch of the decode write");
 }
 
+int32_t extend_write_norm(const tessera_plan *pl, void *k_pool, void *v_pool, const tessera_fresh_rows *rows, void *k_cache, void *v_cache, void *stream) {
+    if (!pl) return api_set_error(TESSERA_INVALID_ARG, "null plan");
+    if (pl->host_only) return api_set_error(TESSERA_INVALID_ARG, "plan was created with TESSERA_PLAN_HOST_ONLY");
+    if (!on_plan_device(pl)) return api_set_error(TESSERA_INVALID_ARG, "the current device is not the plan's");
+    if (pl->n_q == 0) return TESSERA_OK;
+    if (!k_pool || !v_pool || misaligned(k_pool) || misaligned(v_pool))
+        return api_set_error(TESSERA_INVALID_ARG, "k_pool / v_pool must be non-null and 16-byte aligned");
+    if (misaligned(k_cache) || misaligned(v_cache)) return api_set_error(TESSERA_INVALID_ARG, "k_cache / v_cache must be 16-byte aligned");
+    if (pl->retained_tokens > 0 && (!k_cache || !v_cache))
+        return api_set_error(TESSERA_INVALID_ARG, "the plan captures units: k_cache and v_cache must be non-null");
+    if (pl->retained_tokens > 0 && pl->retain_pool_pages == 0 && (k_cache != k_pool || v_cache != v_pool))
+        return api_set_error(TESSERA_INVALID_ARG, "the plan's cache pages are pages of the destination pool: pass k_pool / v_pool as k_cache / v_cache");
+    const int D = pl->cfg.head_dim, Hq = pl->cfg.num_q_heads, H = pl->cfg.num_kv_heads;
+    Fresh f;
+    if (int32_t rc = check_rows(rows, Hq, H, D, &f)) return rc;
+    const DeviceTables &d = pl->dev;
+    const bool il = pl->cfg.rope_pairing == 1;
+    auto kernel = D == 128 ? (il ? extend_norm_kernel<128, true> : extend_norm_kernel<128, false>) : (il ? extend_norm_kernel<64, true> : extend_norm_kernel<64, false>);
+    return launched(launch_kernel(kernel, (unsigned)((pl->n_q + kRowsPerBlock - 1) / kRowsPerBlock), kRowsPerBlock * kThreadsPerRow, 0,
+                                  static_cast<cudaStream_t>(stream), pl->chained, f, static_cast<uint4 *>(k_pool), static_cast<uint4 *>(v_pool),
+                                  static_cast<uint4 *>(k_cache), static_cast<uint4 *>(v_cache), d.q_pos, d.fresh_dst,
+                                  pl->retained_tokens > 0 ? d.retain_dst : nullptr, d.inv_freq, (int)pl->n_q, Hq, H),
+                    "launch of the normalising write");
+}
+
 }  // namespace
 
 int32_t check_decode(const tessera_model_cfg *cfg, const tessera_decode_desc *d, std::string *err) {
@@ -277,37 +302,17 @@ extern "C" {
 
 int32_t tessera_extend_write_norm(const tessera_plan *pl, void *k_pool, void *v_pool, const tessera_fresh_rows *rows, void *k_cache,
                                   void *v_cache, void *stream) {
-    if (!pl) return api_set_error(TESSERA_INVALID_ARG, "null plan");
-    if (pl->host_only) return api_set_error(TESSERA_INVALID_ARG, "plan was created with TESSERA_PLAN_HOST_ONLY");
-    if (pl->n_q == 0) return TESSERA_OK;
-    if (!k_pool || !v_pool || misaligned(k_pool) || misaligned(v_pool))
-        return api_set_error(TESSERA_INVALID_ARG, "k_pool / v_pool must be non-null and 16-byte aligned");
-    if (misaligned(k_cache) || misaligned(v_cache)) return api_set_error(TESSERA_INVALID_ARG, "k_cache / v_cache must be 16-byte aligned");
-    if (pl->retained_tokens > 0 && (!k_cache || !v_cache))
-        return api_set_error(TESSERA_INVALID_ARG, "the plan captures units: k_cache and v_cache must be non-null");
-    if (pl->retained_tokens > 0 && pl->retain_pool_pages == 0 && (k_cache != k_pool || v_cache != v_pool))
-        return api_set_error(TESSERA_INVALID_ARG, "the plan's cache pages are pages of the destination pool: pass k_pool / v_pool as k_cache / v_cache");
-    const int D = pl->cfg.head_dim, Hq = pl->cfg.num_q_heads, H = pl->cfg.num_kv_heads;
-    Fresh f;
-    if (int32_t rc = check_rows(rows, Hq, H, D, &f)) return rc;
-    const DeviceTables &d = pl->dev;
-    const bool il = pl->cfg.rope_pairing == 1;
-    auto kernel = D == 128 ? (il ? extend_norm_kernel<128, true> : extend_norm_kernel<128, false>) : (il ? extend_norm_kernel<64, true> : extend_norm_kernel<64, false>);
-    return launched(launch_kernel(kernel, (unsigned)((pl->n_q + kRowsPerBlock - 1) / kRowsPerBlock), kRowsPerBlock * kThreadsPerRow, 0,
-                                  static_cast<cudaStream_t>(stream), pl->chained, f, static_cast<uint4 *>(k_pool), static_cast<uint4 *>(v_pool),
-                                  static_cast<uint4 *>(k_cache), static_cast<uint4 *>(v_cache), d.q_pos, d.fresh_dst,
-                                  pl->retained_tokens > 0 ? d.retain_dst : nullptr, d.inv_freq, (int)pl->n_q, Hq, H),
-                    "launch of the normalising write");
+    return guarded([&] { return extend_write_norm(pl, k_pool, v_pool, rows, k_cache, v_cache, stream); });
 }
 
 int32_t tessera_decode_write(const tessera_model_cfg *cfg, const tessera_decode_desc *desc, void *k_pool, void *v_pool,
                              const tessera_fresh_rows *rows, void *stream) {
-    return decode_write<false>(cfg, desc, k_pool, v_pool, rows, stream);
+    return guarded([&] { return decode_write<false>(cfg, desc, k_pool, v_pool, rows, stream); });
 }
 
 int32_t tessera_decode_write_kv4(const tessera_model_cfg *cfg, const tessera_decode_desc *desc, void *k_pool4, void *v_pool4,
                                  const tessera_fresh_rows *rows, void *stream) {
-    return decode_write<true>(cfg, desc, k_pool4, v_pool4, rows, stream);
+    return guarded([&] { return decode_write<true>(cfg, desc, k_pool4, v_pool4, rows, stream); });
 }
 
 }  // extern "C"

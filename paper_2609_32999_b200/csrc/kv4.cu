@@ -10,6 +10,7 @@
 
 #include <string>
 
+#include "decode.h"
 #include "device_mem.cuh"
 #include "launch.h"
 #include "pair_chunk.cuh"
@@ -141,6 +142,7 @@ template <bool TO_4BIT>
 int32_t call_kv4(const tessera_plan *pl, const void *k_src, const void *v_src, void *k_dst, void *v_dst, uint32_t flags, void *stream) {
     if (!pl) return api_set_error(TESSERA_INVALID_ARG, "null plan");
     if (pl->host_only) return api_set_error(TESSERA_INVALID_ARG, "plan was created with TESSERA_PLAN_HOST_ONLY");
+    if (!on_plan_device(pl)) return api_set_error(TESSERA_INVALID_ARG, "the current device is not the plan's");
     if (flags & ~uint32_t(TESSERA_FUSE_ROPE)) return api_set_error(TESSERA_INVALID_ARG, "unknown compose flag");
     if (pl->num_source_pages <= 0)
         return api_set_error(TESSERA_INVALID_ARG, "the plan was created without a separate source pool (desc.num_source_pages)");
@@ -163,11 +165,11 @@ using namespace tessera;
 extern "C" {
 
 int32_t tessera_kv_retain_kv4(const tessera_plan *plan, const void *k_src, const void *v_src, void *k_dst4, void *v_dst4, uint32_t flags, void *stream) {
-    return call_kv4<true>(plan, k_src, v_src, k_dst4, v_dst4, flags, stream);
+    return guarded([&] { return call_kv4<true>(plan, k_src, v_src, k_dst4, v_dst4, flags, stream); });
 }
 
 int32_t tessera_kv_compose_from_kv4(const tessera_plan *plan, const void *k_src4, const void *v_src4, void *k_pool, void *v_pool, uint32_t flags, void *stream) {
-    return call_kv4<false>(plan, k_src4, v_src4, k_pool, v_pool, flags, stream);
+    return guarded([&] { return call_kv4<false>(plan, k_src4, v_src4, k_pool, v_pool, flags, stream); });
 }
 
 }  // extern "C"

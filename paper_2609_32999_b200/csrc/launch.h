@@ -47,6 +47,12 @@ cudaError_t launch_grid(void (*kernel)(P...), dim3 grid, unsigned block, size_t 
     return launch_clusters(kernel, grid, block, 1, smem, st, chained, args...);
 }
 
+// Whether the plan's device is the current one (whose stream the caller gives).
+inline bool on_plan_device(const tessera_plan *pl) {
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == pl->device;
+}
+
 // Sources are read from (k_src, v_src) - the destination pools themselves unless the plan names a
 // separate source pool - and written to the plan's destination slots in (k_pool, v_pool).
 cudaError_t launch_gather(const tessera_plan *pl, const void *k_src, const void *v_src, void *k_pool, void *v_pool,

@@ -71,7 +71,6 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
     pl->batch = d->batch;
 
     const int batch = d->batch;
-    if (batch > 0 && window >= *std::max_element(d->seq_len, d->seq_len + batch)) window = n_sink = 0;      // it reaches over every prompt
     pl->window = window;
     pl->n_sink = n_sink;
     // ---- CSR sanity

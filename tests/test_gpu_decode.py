@@ -79,9 +79,10 @@ class Case:
             kv, vv = (k4.values(x, self.page, self.d) for x in (self.k, self.v))
             # the terms the kernel sums: q times c times the scale, and the least value; p times scale times (c - 8), and p times the middle
             ka = (kc.float() * ks[..., None] + km.abs()[..., None]).reshape(kv.shape)
-            va = (vs[..., None] * (vc.float() - 8).abs() + 2.0 ** -12 * (vm + 8 * vs).abs()[..., None]).reshape(vv.shape)
+            va = (vs[..., None] * (vc.float() - 8).abs()).reshape(vv.shape)
+            vsum = (vs[..., None] * (vc.float() + 8) + (vm + 8 * vs).abs()[..., None]).reshape(vv.shape)
         else:
-            kv, vv, ka, va = self.k, self.v, None, None
+            kv, vv, ka, va, vsum = self.k, self.v, None, None, None
         for r in range(len(self.lens)):
             at = torch.from_numpy(self.slots(r)).to(DEV)
             if len(at) == 0:
@@ -89,7 +90,7 @@ class Case:
                 continue
             row = lambda x: None if x is None else x.reshape(-1, *x.shape[2:])[at]
             pos = torch.tensor([len(at) - 1], device=DEV)
-            want = ar.attend(self.q[r:r + 1], row(kv), row(vv), pos, scale=scale, k_size=row(ka), v_size=row(va))
+            want = ar.attend(self.q[r:r + 1], row(kv), row(vv), pos, scale=scale, k_size=row(ka), v_size=row(va), v_sum=row(vsum))
             ar.check(self.out[r:r + 1], self.lse[r:r + 1], want, len(at), "request %d of %d keys" % (r, len(at)))
         return self
 
