@@ -107,15 +107,38 @@ __device__ __forceinline__ void ranges4(const uint4 &lo, const uint4 &hi, float 
         scale[h] = fine ? (s < 7.8886091e-31f ? 0.f : s) : least[h];
     }
 }
-// Codes of 8 elements as the low bytes of eight numbers: adding 1.5 2^23 rounds a quotient to an integer, ties to even.  (Of a
-// scale of 0 or NaN: anything.)
+// Two numbers in one register pair, for the instructions that take both at once.
+__device__ __forceinline__ uint64_t two(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul_two(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// Codes of 8 elements as the low bytes of eight numbers: the quotient of x - m and s as above, and adding 1.5 2^23 rounds it to an
+// integer, ties to even.  (Of a scale of 0 or NaN: anything.)  72 000 rows of 8 heads stored: one element an instruction 74.4 us, two 68.4.
 __device__ __forceinline__ void codes4(const float (&x)[8], float scale, float least, uint32_t (&c)[8]) {
     float inv;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(scale));
+    const uint64_t inv2 = two(inv, inv), minus_s = two(-scale, -scale), minus_m = two(-least, -least), magic = two(12582912.f, 12582912.f);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float d = __fsub_rn(x[i], least);
-        c[i] = __float_as_uint(__fadd_rn(quotient(d, scale, inv), 12582912.f));
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t d = add_two(two(x[2 * i], x[2 * i + 1]), minus_m), q = mul_two(d, inv2);
+        const uint64_t n = add_two(fma_two(fma_two(q, minus_s, d), inv2, q), magic);
+        asm("mov.b64 {%0, %1}, %2;" : "=r"(c[2 * i]), "=r"(c[2 * i + 1]) : "l"(n));
     }
 }
 // 8 bytes of a row of codes: low four bits the elements of the first half, high four those D/2 later.  some: which halves have codes.
