@@ -321,7 +321,7 @@ TESSERA_API int32_t tessera_extend_write(const tessera_plan *plan, void *k_pool,
 typedef struct tessera_fresh_rows {
     const void *q;              /* [n] rows of H_q x D; nullable: keys and values alone                  */
     const void *k, *v;          /* [n] rows of H_kv x D, un-rotated keys; never written                  */
-    void *q_out;                /* [n][H_q][D]; may be q itself where q_row is H_q D                      */
+    void *q_out;                /* [n][H_q][D]; may be q itself where q_row is H_q D, else none of q, k, v lies under it */
     int64_t q_row, k_row, v_row;/* multiples of 8, 0 = H_q D, H_kv D                                     */
     const void *q_weight;       /* [D] weights of the per-head norm of q, respectively k; NULL: that one is  */
     const void *k_weight;       /*     rotated as it is                                                  */

@@ -349,6 +349,7 @@ class Decode:
     they are read by every call when it runs on the GPU, so a step may be captured into a graph.  seq_lens counts the new
     token, whose position is seq_lens - 1; 0 leaves a place out.  `workspace` (uint8, all zeros before its first use; made
     here by default) must not be shared by calls that can overlap on the GPU: use a Decode for each stream or concurrent graph.
+    Keep the object as long as graphs that captured its calls.  Without `workspace` it cannot be made while a graph is captured.
     All tensors live on the device of block_table, which is the current one during the calls."""
 
     def __init__(self, shape, block_table, seq_lens, num_pool_pages: int, window: int = 0, n_sink: int = 0, inv_freq=None, workspace=None):
@@ -371,7 +372,12 @@ class Decode:
         need = ctypes.c_int64(0)
         with torch.cuda.device(self.device):
             _check(_lib.tessera_decode_workspace_bytes(self._args[0], ctypes.byref(need)))
-        self.workspace = torch.zeros(need.value, dtype=torch.uint8, device=self.device) if workspace is None else workspace
+            if workspace is None:
+                if torch.cuda.is_current_stream_capturing():
+                    raise ValueError("a graph is being captured: make the Decode before, or pass a zeroed workspace")
+                workspace = torch.zeros(need.value, dtype=torch.uint8, device=self.device)
+                torch.cuda.current_stream().synchronize()           # (zeros now, for calls on whatever stream)
+        self.workspace = workspace
         _expect("workspace", self.workspace, self._index, torch.uint8, (int(self.workspace.numel()),))
         self._pool = (self.num_pool_pages, shape.page_size, shape.num_kv_heads, d)
         self._pool4 = pool4_shape(shape, self.num_pool_pages)

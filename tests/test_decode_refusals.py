@@ -72,6 +72,13 @@ def test_rows(kw):
     assert tb._lib.tessera_extend_write_norm(plan._h, P, P, ctypes.byref(rows(**kw)), None, None, None) == tb.INVALID_ARG       # (host only)
 
 
+@pytest.mark.parametrize("kw", [dict(q_out=P + 4096), dict(q_out=P + 6128, k=4 * P, v=4 * P), dict(q=3 * P, q_out=P - 6144 + 16), dict(q=3 * P, q_out=P + 1024),
+                                dict(q=3 * P, q_out=P + 1536, v_row=512), dict(q_out=P)])
+def test_q_out_over_rows_that_are_read(kw):
+    """3 rows of 8 + 2 x 2 heads of 128: q 6 144 bytes, k and v 1 536."""
+    assert write(cfg(), desc(), rows(**kw)) == tb.INVALID_ARG and "overlaps" in tb.last_error()
+
+
 def test_rotation():
     assert write(cfg(rope_pairing=2), desc(), rows()) == tb.UNSUPPORTED_SHAPE
     assert write(cfg(rope_theta=0.0), desc(), rows()) == tb.INVALID_ARG
