@@ -21,6 +21,10 @@
 // refreshed only when a row's partial sum would exceed 2^8, so the accumulator in TMEM is rescaled
 // rarely.  Every wait is bounded (ptx::mbar_wait).  A finished tile leaves through a shared-memory
 // output tile and a tiled bulk store.
+// With a window (W) a tile leaves out the item's steps that only the other one sees, and a warp the exponentials of a step that none
+// of its rows sees.  8 prompts of 2 100 to 5 312 tokens, 352 scattered rows each, window 1 024: 101 -> 95 us; 2 of 33 thousand, 1 152
+// rows, window 4 096: 257 -> 248 us (590 TFLOP/s of visible pairs: a pair of tiles goes through 47 steps of which a row sees 33, and the
+// 14 that one tile sees alone take as long as those of both).
 // The kernel is persistent: one thread block per SM walks through its share of the work list, so the
 // barriers, the TMEM allocation and the tensor maps are set up once, and the next item's Q, K and V
 // loads and first S run while the softmax warps still write the previous item's result.
