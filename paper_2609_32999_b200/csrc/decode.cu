@@ -15,7 +15,7 @@
 // before or goes on behind its stretch is a part; at the end the block joins its warps' parts, and parts of pairs that
 // leave the block go to the workspace, where the last block to arrive joins them, always in the order of the tiles.
 // (Blocks that took pairs in turn, all their warps on one, and met at the end of each: 215 us where 64 requests of 200 to
-// 16 384 tokens, 8 heads in 4 bits, take 130 us; a join in a kernel of its own: 4 us more for any batch.)
+// 16 384 tokens, 8 heads in 4 bits, took 130 us, now 123; a join in a kernel of its own: 4 us more for any batch.)
 // A row that is not visible, past the end or on a page outside the pool is filled with zeros and never read, so what stands
 // there does not matter.
 #include <cmath>
@@ -733,9 +733,11 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                         }
                 }
                 if constexpr (F4) {
-                    // sum p v = sum (p s) (c - 8) + sum p (m + 8 s), half by half.  p s v_unit is the MMA's operand, rounded to bf16; a code in the
-                    // last four bits of a half is the bf16 number c 2^-133 (16 c 2^-133 one nibble higher), a subnormal that needs no
-                    // conversion, and -8 of all of them is one more product with the same operand.
+                    // sum p v = sum b (c - 8) + sum p (m + 8 s), half by half, with b = p s rounded to bf16 (in units of 1 / v_unit), the MMA's
+                    // operand; a code in the last four bits of a half is the bf16 number c 2^-133 (16 c 2^-133 one nibble higher), a
+                    // subnormal that needs no conversion.  The MMAs sum b c; -8 b of the lane's own keys joins p (m + 8 s), so that b's rounding
+                    // counts for the distance from the middle alone.
+                    const float eight = __uint_as_float((257u << 23) - __float_as_uint(v_unit));           // 8 / v_unit, a power of two
                     if (!FOLD || sub == 0) {
                         const int u = FOLD ? 0 : sub;
 #pragma unroll
@@ -747,9 +749,11 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                                 const float su = vs[half] * v_unit;
 #pragma unroll
                                 for (int n = 0; n < NQ; ++n) {
-                                    weight[n][half][i] = transposed(pack_bf16(p[u][n][2 * i] * su, p[u][n][2 * i + 1] * su));
+                                    const uint32_t b = pack_bf16(p[u][n][2 * i] * su, p[u][n][2 * i + 1] * su);
+                                    weight[n][half][i] = transposed(b);
 #pragma unroll
-                                    for (int e = 0; e < 2; ++e) off[n][half][e] = fmaf(p[u][n][2 * i + e], mid[half], off[n][half][e]);
+                                    for (int e = 0; e < 2; ++e)
+                                        off[n][half][e] = fmaf(p[u][n][2 * i + e], mid[half], fmaf(-eight, __uint_as_float(e ? b & 0xffff0000u : b << 16), off[n][half][e]));
                                 }
                             }
                         }
@@ -781,12 +785,11 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                                 for (int i = 0; i < 2; ++i) pr[jj][i] = __byte_perm(w[2 * i][x], w[2 * i + 1][x], 0x0400 + (2 * jp + jj) * 0x0101);
 #pragma unroll
                             for (int half = 0; half < 2; ++half) {
-                                const uint32_t bits = half ? 0x00f000f0u : 0x000f000fu, eight = half ? 0x80808080u : 0x80088008u;
-                                const uint32_t f[4] = {pr[0][0] & bits, pr[1][0] & bits, pr[0][1] & bits, pr[1][1] & bits}, minus[4] = {eight, eight, eight, eight};
+                                const uint32_t bits = half ? 0x00f000f0u : 0x000f000fu;
+                                const uint32_t f[4] = {pr[0][0] & bits, pr[1][0] & bits, pr[0][1] & bits, pr[1][1] & bits};
 #pragma unroll
                                 for (int n = 0; n < NQ; ++n) {
                                     float(&to)[4] = acc[n][(half * (D / 64) + x) * 2 + jp];
-                                    mma(to, minus, b[n][half][0], b[n][half][1]);
                                     mma(to, f, b[n][half][0], b[n][half][1]);
                                 }
                             }
