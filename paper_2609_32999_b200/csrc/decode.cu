@@ -15,7 +15,7 @@
 // before or goes on behind its stretch is a part; at the end the block joins its warps' parts, and parts of pairs that
 // leave the block go to the workspace, where the last block to arrive joins them, always in the order of the tiles.
 // (Blocks that took pairs in turn, all their warps on one, and met at the end of each: 215 us where 64 requests of 200 to
-// 16 384 tokens, 8 heads in 4 bits, took 130 us, now 123; a join in a kernel of its own: 4 us more for any batch.)
+// 16 384 tokens, 8 heads in 4 bits, then took 130 us, now 113; a join in a kernel of its own: 4 us more for any batch.)
 // A row that is not visible, past the end or on a page outside the pool is filled with zeros and never read, so what stands
 // there does not matter.
 #include <cmath>
@@ -60,7 +60,8 @@ struct Args {
 // Shared memory: every warp's ring (a stage: the rows of a tile of K, of V and, 4-bit, their numbers) and its part of the pair that
 // its stretch begins in; the part of the one it ends in goes into the ring.
 template <int D, bool F4, int NQ> struct Geo {
-    // (4-bit: 16 warps of 128 registers 135 us, 12 of 168 130, 8 144: 64 requests of up to 16 384 tokens, 8 heads)
+    // (4-bit, 64 requests of up to 16 384 tokens, 8 heads: 12 warps of 168 registers 113 us, with a third stage 112 but a lone request
+    // 12.0 -> 12.5; 16 of 128 115, 14 127.  Two fifths of the instructions spread codes over operands; their pipe is busy 56 % of the time.)
     static constexpr int kWarps = F4 && NQ == 1 ? 12 : 8;
     static constexpr int kThreads = 32 * kWarps;
     static constexpr int kTile = F4 ? 32 : 16;                            // keys
@@ -235,7 +236,7 @@ __device__ __forceinline__ void empty_requests(const Args &a) {
 
 // SMALL: pages of fewer tokens than a tile.  FOLD (4-bit, at most 4 queries a KV head): columns 4 to 7 hold the same queries as 0 to
 // 3, and stand for the tile's second 16 keys where 0 to 3 stand for the first: a lane has half the scores to turn into weights, none
-// of them of an empty column.  The two sets of columns, each with a reference of its own, come together when the pair ends.
+// of them of an empty column.  In the output they are the second half of head_dim (see the values' products).
 template <int D, bool F4, int NQ, bool SMALL, bool FOLD>
 __global__ void __launch_bounds__(Geo<D, F4, NQ>::kThreads, 1)
 decode_attn_kernel(const __grid_constant__ Args a) {
@@ -285,14 +286,15 @@ decode_attn_kernel(const __grid_constant__ Args a) {
         const uint32_t row_bytes = F4 ? (uint32_t)G::kRow : a.H_kv * head_bytes, page_bytes = F4 ? a.H_kv * head_bytes : row_bytes << page_shift;
         const uint32_t numbers = (uint32_t)a.page_size * (D / 2);
         // A lane's own places: of its 16 bytes of a turn's rows (and its 8 of their numbers) in the keys of page 0, head h, and in a stage.  16-bit
-        // chunks are turned by the row, as ldmatrix wants them; of 4-bit values the halves of rows 4-7 of 8 change places, so that
-        // the four rows and eight columns that a warp's lanes ask for at once lie in different banks.
+        // chunks are turned by the row, as ldmatrix wants them; so are those of 4-bit values, of two rows (head_dim 64: four) alike,
+        // so that 8 rows' lie in different banks.
         const uint32_t place = lane / CPR * row_bytes + lane % CPR * 16;
         const uint8_t *lane_k = a.k + (size_t)h * head_bytes + place;
         const ptrdiff_t to_v = a.v - a.k;
         const int32_t to_numbers = (int32_t)(numbers + lane * 8) - (int32_t)place;
         auto chunk_k = [&](int row) { return F4 ? lane % CPR : (lane % CPR) ^ (row & 7); };
-        auto chunk_v = [&](int row) { return F4 && D == 128 ? (lane % CPR) ^ (((row >> 2) & 1) << 1) : chunk_k(row); };
+        auto turned_v = [](int chunk, int row) { return chunk ^ (D == 128 ? (row >> 1) & 3 : (row >> 2) & 1); };
+        auto chunk_v = [&](int row) { return F4 ? turned_v(lane % CPR, row) : chunk_k(row); };
         int run = 0;                               // tiles from j on that are neither first nor last of their pair and all there, pages apart
         uint32_t plain = 0;                        // stages that hold such a tile
         auto fetch = [&](int at) {
@@ -379,7 +381,8 @@ decode_attn_kernel(const __grid_constant__ Args a) {
         float q_sum[NQ][2][2];           // 4-bit: sums of q over each half, of columns 2 t and 2 t + 1, in units of `unit`
         float unit[NQ][2];               // score times scale log2(e) per score sum: scale_log2, 4-bit: by column, for q's and the codes' scaling
         float m[NQ][2], l[NQ][2], off[NQ][2][2];         // off (4-bit): sums of p times a half's middle value
-        float acc[NQ][D / 16][4];        // 4-bit: times v_unit 2^-133, second half 2^-129
+        constexpr int NA = FOLD ? D / 32 : D / 16;
+        float acc[NQ][NA][4];            // 4-bit: times v_unit 2^-133, second half 2^-129 (FOLD: lanes of columns 4 to 7)
         float v_unit = kValueUnit, v_limit = kValueTop / kValueUnit;
 
         auto begin_pair = [&](int pair) {
@@ -451,26 +454,13 @@ decode_attn_kernel(const __grid_constant__ Args a) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) m[n][e] = -INFINITY, l[n][e] = off[n][0][e] = off[n][1][e] = 0.f;
 #pragma unroll
-                for (int d = 0; d < D / 16; ++d)
+                for (int d = 0; d < NA; ++d)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[n][d][e] = 0.f;
             }
         };
         // Sums over the lanes of a column, and (4-bit) the middle values' share into the accumulators.
         auto sum_up = [&]() {
-            if constexpr (FOLD) {              // columns c and c + 4 (lanes t and t + 2) to one reference, and together
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float ref = fmaxf(m[0][e], __shfl_xor_sync(0xffffffffu, m[0][e], 2)), f = m[0][e] == -INFINITY ? 0.f : ex2(m[0][e] - ref);
-                    m[0][e] = ref;
-                    auto both = [&](float x) { return x * f + __shfl_xor_sync(0xffffffffu, x * f, 2); };
-                    l[0][e] = both(l[0][e]);
-                    off[0][0][e] = both(off[0][0][e]);
-                    off[0][1][e] = both(off[0][1][e]);
-#pragma unroll
-                    for (int d = 0; d < D / 16; ++d) acc[0][d][e] = both(acc[0][d][e]), acc[0][d][e + 2] = both(acc[0][d][e + 2]);
-                }
-            }
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -478,24 +468,29 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                     auto column_sum = [](float x) {
                         x += __shfl_xor_sync(0xffffffffu, x, 4);
                         x += __shfl_xor_sync(0xffffffffu, x, 8);
-                        return x + __shfl_xor_sync(0xffffffffu, x, 16);
+                        x += __shfl_xor_sync(0xffffffffu, x, 16);
+                        return FOLD ? x + __shfl_xor_sync(0xffffffffu, x, 2) : x;          // (columns c and c + 4: lanes t and t + 2)
                     };
                     l[n][e] = column_sum(l[n][e]);
                     if constexpr (F4) {
                         const float o[2] = {column_sum(off[n][0][e]), column_sum(off[n][1][e])};
                         const float back = kValueUnit / v_unit;
 #pragma unroll
-                        for (int d = 0; d < D / 16; ++d)
+                        for (int d = 0; d < NA; ++d) {
+                            const bool second = FOLD ? t >= 2 : d >= D / 32;
 #pragma unroll
                             for (int i = 0; i < 2; ++i)          // 2^133 / v_unit, 2^129 / v_unit
-                                acc[n][d][e + 2 * i] = fmaf(acc[n][d][e + 2 * i] * (d < D / 32 ? 5.9029581035870565e20f : 3.6893488147419103e19f), back, o[d / (D / 32)]);
+                                acc[n][d][e + 2 * i] = fmaf(acc[n][d][e + 2 * i] * (second ? 3.6893488147419103e19f : 5.9029581035870565e20f), back, second ? o[1] : o[0]);
+                        }
                     }
                 }
         };
         // Element of head_dim that row quad (i = 0) or quad + 8 (i = 1) of accumulator d is.
         auto element = [&](int d, int i) {
-            return F4 ? d / (D / 32) * (D / 2) + (D / 16) * quad + d / 2 % (D / 64) * 4 + d % 2 * 2 + i : 16 * d + 8 * i + quad;
+            return F4 ? (FOLD ? t >> 1 : d / (D / 32)) * (D / 2) + d % (D / 32) * 16 + 2 * quad + i : 16 * d + 8 * i + quad;
         };
+        // Query (of the KV head) whose column a lane's accumulators 0 and 2, respectively 1 and 3, are.
+        auto column = [&](int n, int e) { return FOLD ? (2 * t + e) & 3 : n * 8 + 2 * t + e; };
         auto write_out = [&](int pair) {
             const size_t head0 = (size_t)(pair / a.H_kv) * a.H_q + pair % a.H_kv * a.g;
 #pragma unroll
@@ -503,24 +498,18 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                 float inv[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int col = n * 8 + 2 * t + e;
+                    const int col = column(n, e);
                     inv[e] = m[n][e] == -INFINITY ? 0.f : 1.f / l[n][e];
-                    if (a.lse && quad == 0 && col < a.g) a.lse[head0 + col] = m[n][e] == -INFINITY ? -INFINITY : (m[n][e] + log2f(l[n][e])) * 0.6931471805599453f;
+                    if (a.lse && quad == 0 && col < a.g && (!FOLD || t < 2)) a.lse[head0 + col] = m[n][e] == -INFINITY ? -INFINITY : (m[n][e] + log2f(l[n][e])) * 0.6931471805599453f;
                 }
                 if constexpr (F4) {
-                    // a lane has D / 16 elements side by side of both halves
+                    // (accumulators e and e + 2 are neighbouring elements)
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
-                        if (n * 8 + 2 * t + e < a.g)
+                        if (column(n, e) < a.g)
 #pragma unroll
-                            for (int half = 0; half < 2; ++half) {
-                                uint32_t *o = reinterpret_cast<uint32_t *>(a.out + (head0 + n * 8 + 2 * t + e) * D + half * (D / 2) + (D / 16) * quad);
-                                uint32_t y[D / 32];
-#pragma unroll
-                                for (int d = 0; d < D / 32; ++d) y[d] = pack_bf16(acc[n][half * (D / 32) + d][e] * inv[e], acc[n][half * (D / 32) + d][e + 2] * inv[e]);
-                                if constexpr (D == 128) *reinterpret_cast<uint4 *>(o) = make_uint4(y[0], y[1], y[2], y[3]);
-                                else *reinterpret_cast<uint2 *>(o) = make_uint2(y[0], y[1]);
-                            }
+                            for (int d = 0; d < NA; ++d)
+                                *reinterpret_cast<uint32_t *>(a.out + (head0 + column(n, e)) * D + element(d, 0)) = pack_bf16(acc[n][d][e] * inv[e], acc[n][d][e + 2] * inv[e]);
                 } else {
                     // 8 x 8 blocks turned, so that a lane has two neighbouring elements of one query
                     const int col = n * 8 + quad;
@@ -539,10 +528,10 @@ decode_attn_kernel(const __grid_constant__ Args a) {
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int col = n * 8 + 2 * t + e;
+                    const int col = column(n, e);
                     if (quad == 0) s_ml[warp][which][col] = make_float2(m[n][e], l[n][e]);
 #pragma unroll
-                    for (int d = 0; d < D / 16; ++d) {
+                    for (int d = 0; d < NA; ++d) {
                         to[col * RP + element(d, 0)] = acc[n][d][e];
                         to[col * RP + element(d, 1)] = acc[n][d][e + 2];
                     }
@@ -568,9 +557,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
             }
             const uint32_t kb = ring + at * G::kStageBytes, vb = kb + T * G::kRow;
             const uint8_t *kp8 = smem + (kb - smem0), *vp8 = smem + (vb - smem0);
-            // rows of a score tile: natural keys of the 16, 4-bit: row i is key i ^ (i / 2 % 2) (see the bank note above)
-            const int row0 = F4 ? quad ^ ((quad >> 1) & 1) : quad;
-            auto key_row = [&](int u, int i) { return (FOLD ? t >> 1 : u) * 16 + row0 + 8 * i; };      // of the tile, of a lane's scores 2 i and 2 i + 1
+            auto key_row = [&](int u, int i) { return (FOLD ? t >> 1 : u) * 16 + quad + 8 * i; };      // of the tile, of a lane's scores 2 i and 2 i + 1
             float sc[SC][NQ][4];
             if constexpr (F4) {
                 float part[SC][NQ][2][4];
@@ -581,10 +568,10 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                     for (int n = 0; n < NQ; ++n)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) sum[n][0][e] = sum[n][1][e] = 0.f;
-                    uint32_t w[2][D / 32];               // 16 (8) bytes of rows row0 and row0 + 8
+                    uint32_t w[2][D / 32];               // 16 (8) bytes of rows quad and quad + 8
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const uint8_t *b = kp8 + (sub * 16 + row0 + 8 * i) * G::kRow + (D / 8) * t;
+                        const uint8_t *b = kp8 + (sub * 16 + quad + 8 * i) * G::kRow + (D / 8) * t;
                         if constexpr (D == 128) *reinterpret_cast<uint4 *>(w[i]) = *reinterpret_cast<const uint4 *>(b);
                         else *reinterpret_cast<uint2 *>(w[i]) = *reinterpret_cast<const uint2 *>(b);
                     }
@@ -687,12 +674,12 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                     if ((top > v_limit || (begins && top > 0.f)) && top < INFINITY) {
                         // 2^(64 - exponent of top), where there is something already 2^(100 - exponent), at most 2^120
                         const float to = __uint_as_float((uint32_t)min((begins ? 64 : 100) + 254 - (int)(__float_as_uint(top) >> 23), 247) << 23);
-                    const float f = to / v_unit;
+                        const float f = to / v_unit;
                         v_unit = to, v_limit = kValueTop / to;
 #pragma unroll
                         for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                            for (int d = 0; d < D / 16; ++d)
+                            for (int d = 0; d < NA; ++d)
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) acc[n][d][e] *= f;
                     }
@@ -707,19 +694,21 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                        if (FOLD) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                         const float mn = fmaxf(m[n][e], top), f = mn == -INFINITY ? 1.f : ex2(m[n][e] - mn), ref = mn == -INFINITY ? 0.f : mn;
                         m[n][e] = mn;
                         l[n][e] *= f;
                         off[n][0][e] *= f;
                         off[n][1][e] *= f;
 #pragma unroll
-                        for (int d = 0; d < D / 16; ++d) acc[n][d][e] *= f, acc[n][d][e + 2] *= f;
+                        for (int d = 0; d < NA; ++d) acc[n][d][e] *= f, acc[n][d][e + 2] *= f;
 #pragma unroll
                         for (int u = 0; u < SC; ++u)
 #pragma unroll
                             for (int i = 0; i < 2; ++i) p[u][n][e + 2 * i] = fmaf(sc[u][n][e + 2 * i], unit[n][e], -ref);
                     }
             }
+            uint32_t other[2];                   // (FOLD) the weights of the lane 16 away: the other half's, of the other 16 keys
             uint32_t weight[NQ][2][2];           // (4-bit) the second operand of the values' products, by half and by rows quad and quad + 8
 #pragma unroll
             for (int sub = 0; sub < SUB; ++sub) {
@@ -758,42 +747,44 @@ decode_attn_kernel(const __grid_constant__ Args a) {
                             }
                         }
                     }
+                    // Without FOLD a product for each half.  FOLD: columns 0 to 3 are the first half of the 16 keys' values, 4 to 7 the second.  Bytes
+                    // as they are, 16 c1 + c0, stand against the first half's weights; the second codes alone, 16 c1, against the second
+                    // half's and, to take them off again, minus the first's.  (255 2^-133 is a bf16 number yet.)
                     uint32_t b[NQ][2][2];
 #pragma unroll
                     for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                        for (int half = 0; half < 2; ++half)
+                        for (int i = 0; i < 2; ++i)
+                            if constexpr (FOLD) {
+                                if (sub == 0) other[i] = __shfl_xor_sync(0xffffffffu, quad < 4 ? weight[n][1][i] : weight[n][0][i], 16);
+                                const uint32_t mine = sub == 0 ? (quad < 4 ? weight[n][0][i] : other[i]) : (quad < 4 ? other[i] : weight[n][1][i]);
+                                b[n][0][i] = quad < 4 ? mine : 0u;
+                                b[n][1][i] = quad < 4 ? mine ^ 0x80008000u : mine;
+                            } else {
+                                b[n][0][i] = weight[n][0][i], b[n][1][i] = weight[n][1][i];
+                            }
+                    // 8 x 8 blocks of pairs of bytes, turned: a lane has bytes 2 quad and 2 quad + 1 of 16 of the keys of operand rows 2 t and 2 t + 1
+                    // (respectively 8 more), whose even and odd bytes are the products' rows quad and quad + 8.
+                    const int row = sub * 16 + (lane & 15);
+                    const uint32_t from = vb + row * G::kRow;
 #pragma unroll
-                            for (int i = 0; i < 2; ++i) b[n][half][i] = FOLD && quad / 4 != sub ? 0u : weight[n][half][i];
-                    // keys of operand rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9, and of each the bytes whose elements this lane's rows of V^T are
-                    uint32_t w[4][D / 64];
+                    for (int c = 0; c < D / 32; c += 2) {
+                        uint32_t w[4];
+                        ldmatrix_x4_trans(w, from + turned_v(c + (lane >> 4), row) * 16);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int op = 2 * t + (i & 1), row = sub * 16 + (i >> 1) * 8 + (op ^ ((op >> 1) & 1));
-                        const uint8_t *p8 = vp8 + row * G::kRow;
-                        if constexpr (D == 128) *reinterpret_cast<uint2 *>(w[i]) = *reinterpret_cast<const uint2 *>(p8 + ((quad * 8) ^ (((row >> 2) & 1) << 5)));
-                        else w[i][0] = *reinterpret_cast<const uint32_t *>(p8 + quad * 4);
-                    }
+                        for (int x = 0; x < 2; ++x) {
+                            const uint32_t w0 = w[2 * x], w1 = w[2 * x + 1];
+                            // (FOLD: the bytes, else the first half's codes; the odd ones a byte lower)
+                            const uint32_t mask = FOLD ? 0x00ff00ffu : 0x000f000fu, u0 = FOLD ? __byte_perm(w0, 0, 0x4341) : w0 >> 8, u1 = FOLD ? __byte_perm(w1, 0, 0x4341) : w1 >> 8;
+                            const uint32_t lo[4] = {w0 & mask, FOLD ? u0 : u0 & mask, w1 & mask, FOLD ? u1 : u1 & mask};
+                            const uint32_t hi[4] = {w0 & 0x00f000f0u, u0 & 0x00f000f0u, w1 & 0x00f000f0u, u1 & 0x00f000f0u};
 #pragma unroll
-                    for (int x = 0; x < D / 64; ++x)
-#pragma unroll
-                        for (int jp = 0; jp < 2; ++jp) {
-                            uint32_t pr[2][2];                // byte 2 jp + j of two keys, operand rows 2 i and 2 i + 1 of the four
-#pragma unroll
-                            for (int jj = 0; jj < 2; ++jj)
-#pragma unroll
-                                for (int i = 0; i < 2; ++i) pr[jj][i] = __byte_perm(w[2 * i][x], w[2 * i + 1][x], 0x0400 + (2 * jp + jj) * 0x0101);
-#pragma unroll
-                            for (int half = 0; half < 2; ++half) {
-                                const uint32_t bits = half ? 0x00f000f0u : 0x000f000fu;
-                                const uint32_t f[4] = {pr[0][0] & bits, pr[1][0] & bits, pr[0][1] & bits, pr[1][1] & bits};
-#pragma unroll
-                                for (int n = 0; n < NQ; ++n) {
-                                    float(&to)[4] = acc[n][(half * (D / 64) + x) * 2 + jp];
-                                    mma(to, f, b[n][half][0], b[n][half][1]);
-                                }
+                            for (int n = 0; n < NQ; ++n) {
+                                mma(acc[n][c + x], lo, b[n][0][0], b[n][0][1]);
+                                mma(acc[n][(FOLD ? 0 : D / 32) + c + x], hi, b[n][1][0], b[n][1][1]);
                             }
                         }
+                    }
                 } else {
                     uint32_t b[NQ][2];
 #pragma unroll

@@ -80,7 +80,11 @@ class Case:
             # the terms the kernel sums: q times c times the scale, and the least value; p times scale times (c - 8), and p times the middle
             ka = (kc.float() * ks[..., None] + km.abs()[..., None]).reshape(kv.shape)
             va = (vs[..., None] * (vc.float() - 8).abs()).reshape(vv.shape)
-            vsum = (vs[..., None] * (vc.float() + 8) + (vm + 8 * vs).abs()[..., None]).reshape(vv.shape)
+            # (with at most 4 queries a KV head the first half's codes come as bytes less the second's: c0 + 16 c1 - 16 c1, and -8, the middle)
+            taken_off = torch.zeros_like(vc, dtype=torch.float32)
+            if self.q.shape[1] <= 4 * ks.shape[2]:
+                taken_off[..., 0, :] = 32 * vc[..., 1, :].float()
+            vsum = (vs[..., None] * (vc.float() + taken_off + 8) + (vm + 8 * vs).abs()[..., None]).reshape(vv.shape)
         else:
             kv, vv, ka, va, vsum = self.k, self.v, None, None, None
         for r in range(len(self.lens)):
