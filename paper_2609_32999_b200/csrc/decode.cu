@@ -81,6 +81,16 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float lg2(float x) {                      // 2^-22 off between 1/2 and 2, elsewhere an ulp or so
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float about_one_over(float x) {           // 1 ulp
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -133,21 +143,30 @@ __device__ __forceinline__ Visible visible(int len, const Args &a) {
 // Of a stage: whether the tile is its pair's first and last.
 constexpr uint32_t kFirst = 1, kLast = 2;
 
-// A pair: its number, tiles of the batch before its first, its tiles (of a warp's part: < 0, there is none).
+// A pair: its number (its first query's row is g times that), tiles of the batch before its first, its tiles (of a warp's part: < 0, there is none).
 struct Pair { int pair, begin, tiles; };
 
-// Worker i of the batch has the tiles from all i / workers (rounded down) on.
-__device__ __forceinline__ int first_tile(int i, int workers, int all) {
-    const uint32_t whole = (uint32_t)all / (uint32_t)workers, rest = (uint32_t)all % (uint32_t)workers;       // (rest i < 2^32: 65 536 workers)
-    return (int)(whole * (uint32_t)i + rest * (uint32_t)i / (uint32_t)workers);
-}
-// The worker of tile x: the largest i with first_tile(i) <= x.
-__device__ __forceinline__ int worker_of(int x, int workers, int all) {
-    int i = min(workers - 1, (int)((float)x * (float)workers / (float)all));           // (two too low or high at most)
-    while (first_tile(i, workers, all) > x) --i;
-    while (i + 1 < workers && first_tile(i + 1, workers, all) <= x) ++i;
-    return i;
-}
+// `all` tiles shared out to workers: worker i has those from all i / workers (rounded down) on.  At most 16 384 workers.
+struct Shares {
+    int workers, all;
+    uint32_t whole, rest;
+    float one;           // of a worker
+    __device__ __forceinline__ Shares(int n, int tiles) : workers(n), all(tiles), whole((uint32_t)tiles / (uint32_t)n), rest((uint32_t)tiles - whole * (uint32_t)n), one(about_one_over((float)n)) {}
+    __device__ __forceinline__ int first(int i) const {
+        // rest i / workers, a quotient below 2^14 of a number below 2^28: by its reciprocal one off at most (an integer division takes 100
+        // cycles, and a lone request waits for several in a row)
+        const uint32_t n = rest * (uint32_t)i, q = (uint32_t)((float)n * one);
+        const int left = (int)(n - q * (uint32_t)workers);
+        return (int)(whole * (uint32_t)i + q) + (left >= workers) - (left < 0);
+    }
+    // The worker of tile x: the largest i with first(i) <= x.
+    __device__ __forceinline__ int of(int x) const {
+        int i = min(workers - 1, (int)((float)x * (float)workers / (float)all));           // (two too low or high at most)
+        while (first(i) > x) --i;
+        while (i + 1 < workers && first(i + 1) <= x) ++i;
+        return i;
+    }
+};
 
 // A warp's stretch of the batch's `all` tiles: [first, last), beginning in request r, before which lie `before` tiles.  Every warp sums the
 // batch by itself, a stretch of the requests a lane: no waiting for others, and the lengths are in L1 after the first.
@@ -161,6 +180,7 @@ __device__ __forceinline__ Stretch stretch_of(const Args &a, int few) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, per = (a.batch + 31) / 32, r0 = lane * per, r1 = min(a.batch, r0 + per);
     auto tiles = [&](int r) { return visible<T>(a.seq_len[r], a).n; };
     int own = 0, some = 0, most = 0;                  // tiles, requests that have any, tiles of a head of the longest
+#pragma unroll 2
     for (int r = r0; r < r1; ++r) {
         const int n = tiles(r);
         own += n * a.H_kv, some += n > 0, most = max(most, n);
@@ -190,34 +210,42 @@ __device__ __forceinline__ Stretch stretch_of(const Args &a, int few) {
     Stretch s;
     s.all = __shfl_sync(0xffffffffu, end, 31);
     const int grid = (int)gridDim.x, pairs = __shfl_sync(0xffffffffu, count, 31) * a.H_kv;
-    const bool whole = (int64_t)((pairs + grid - 1) / grid) * most <= few + s.all / grid;
+    const float a_block = about_one_over((float)grid);         // (a rule of thumb, the same for every warp)
+    const bool whole = ceilf((float)pairs * a_block) * (float)most <= (float)few + (float)s.all * a_block;
     s.workers = min(grid * NW, s.all);
     s.first = s.last = s.all;
     s.r = s.before = 0;
     const int blocks = min(grid, pairs);
     if (whole ? (int)blockIdx.x >= blocks : (int)blockIdx.x * NW + warp >= s.workers) return s;       // (fewer tiles than warps: the first have one each)
     if (whole) {
-        int first, last;
-        if (pairs <= grid) {                           // a pair each
-            find((int)blockIdx.x / a.H_kv, false, s.r, s.before);
-            const int n = tiles(s.r);
-            first = s.before + (int)blockIdx.x % a.H_kv * n, last = first + n;
-        } else {
-            auto first_of = [&](int pair) {            // the pair's first tile
-                if (pair == pairs) return s.all;
-                int r, before;
-                find(pair / a.H_kv, false, r, before);
-                return before + pair % a.H_kv * tiles(r);
-            };
-            first = first_of(first_tile(blockIdx.x, blocks, pairs)), last = first_of(first_tile(blockIdx.x + 1, blocks, pairs));
+        const Shares pair_shares(blocks, pairs);
+        int first = 0, last = 0;
+#pragma unroll 1                                           // (one copy of the search: see the note at the joins)
+        for (int end = 0; end < 2; ++end) {
+            const int pair = pairs <= grid ? (int)blockIdx.x : pair_shares.first((int)blockIdx.x + end);
+            int r = 0, x = s.all, n = 0;
+            if (pair < pairs) {
+                const int nth = pair / a.H_kv;
+                find(nth, false, r, x);
+                n = tiles(r);
+                s.r = r, s.before = x;
+                x += (pair - nth * a.H_kv) * n;
+            }
+            (end ? last : first) = x;
+            if (pairs <= grid) {
+                last = first + n;
+                break;
+            }
         }
         const int mates = min(NW, last - first);
-        s.first = warp < mates ? first + first_tile(warp, mates, last - first) : last;
-        s.last = warp < mates ? first + first_tile(warp + 1, mates, last - first) : last;
+        const Shares shares(mates, last - first);
+        s.first = warp < mates ? first + shares.first(warp) : last;
+        s.last = warp < mates ? first + shares.first(warp + 1) : last;
         if (warp >= mates || pairs <= grid) return s;
     } else {
-        s.first = first_tile((int)blockIdx.x * NW + warp, s.workers, s.all);
-        s.last = first_tile((int)blockIdx.x * NW + warp + 1, s.workers, s.all);
+        const Shares shares(s.workers, s.all);
+        s.first = shares.first((int)blockIdx.x * NW + warp);
+        s.last = shares.first((int)blockIdx.x * NW + warp + 1);
     }
     find(s.first, true, s.r, s.before);
     return s;
@@ -226,10 +254,13 @@ __device__ __forceinline__ Stretch stretch_of(const Args &a, int few) {
 // Requests without a key: zeros, and nothing for a sum.
 template <int D, int NT, int T>
 __device__ __forceinline__ void empty_requests(const Args &a) {
+#pragma unroll 1
     for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
         if (visible<T>(a.seq_len[r], a).n == 0) {
+#pragma unroll 1
             for (int i = threadIdx.x; i < a.H_q * D / 8; i += NT) stg(reinterpret_cast<uint4 *>(a.out + (size_t)r * a.H_q * D) + i, make_uint4(0, 0, 0, 0));
             if (a.lse)
+#pragma unroll 1
                 for (int i = threadIdx.x; i < a.H_q; i += NT) a.lse[(size_t)r * a.H_q + i] = -INFINITY;
         }
 }
@@ -386,12 +417,11 @@ decode_attn_kernel(const __grid_constant__ Args a) {
         float v_unit = kValueUnit, v_limit = kValueTop / kValueUnit;
 
         auto begin_pair = [&](int pair) {
-            const int qr = pair / a.H_kv, qh = pair - qr * a.H_kv;
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
                 const int col = n * 8 + (FOLD ? quad & 3 : quad);
                 const bool there = col < a.g;
-                const __nv_bfloat16 *q = a.q + ((size_t)qr * a.H_q + qh * a.g + (there ? col : 0)) * D;
+                const __nv_bfloat16 *q = a.q + ((size_t)pair * a.g + (there ? col : 0)) * D;
                 if constexpr (F4) {
                     // A code in the last four bits of a half is the fp16 number c 2^-24 (16 c 2^-24 one nibble higher), so keys need no
                     // conversion where q is fp16: scaled by a power of two for its greatest element to lie below 2^14, the second
@@ -492,15 +522,15 @@ decode_attn_kernel(const __grid_constant__ Args a) {
         // Query (of the KV head) whose column a lane's accumulators 0 and 2, respectively 1 and 3, are.
         auto column = [&](int n, int e) { return FOLD ? (2 * t + e) & 3 : n * 8 + 2 * t + e; };
         auto write_out = [&](int pair) {
-            const size_t head0 = (size_t)(pair / a.H_kv) * a.H_q + pair % a.H_kv * a.g;
+            const size_t head0 = (size_t)pair * a.g;
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
                 float inv[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int col = column(n, e);
-                    inv[e] = m[n][e] == -INFINITY ? 0.f : 1.f / l[n][e];
-                    if (a.lse && quad == 0 && col < a.g && (!FOLD || t < 2)) a.lse[head0 + col] = m[n][e] == -INFINITY ? -INFINITY : (m[n][e] + log2f(l[n][e])) * 0.6931471805599453f;
+                    inv[e] = m[n][e] == -INFINITY ? 0.f : about_one_over(l[n][e]);
+                    if (a.lse && quad == 0 && col < a.g && (!FOLD || t < 2)) a.lse[head0 + col] = m[n][e] == -INFINITY ? -INFINITY : (m[n][e] + lg2(l[n][e])) * 0.6931471805599453f;
                 }
                 if constexpr (F4) {
                     // (accumulators e and e + 2 are neighbouring elements)
@@ -540,15 +570,16 @@ decode_attn_kernel(const __grid_constant__ Args a) {
         };
 
         begin_pair(r * a.H_kv + h);           // (q comes in beside the page ids)
-#pragma unroll
-        for (int s = 0; s < G::kStages - 1; ++s) fetch(s);
         bool begun_here = false;
         Pair now{};
         int at = 0;
-        for (int s = 0; s < my_tiles; ++s) {
-            cp_wait<G::kStages - 2>();
-            __syncwarp();
-            fetch(at == 0 ? G::kStages - 1 : at - 1);      // into the stage consumed in the last turn
+        for (int s = 1 - G::kStages; s < my_tiles; ++s) {
+            if (s >= 0) {
+                cp_wait<G::kStages - 2>();
+                __syncwarp();
+            }
+            fetch(s < 0 ? s + G::kStages - 1 : at == 0 ? G::kStages - 1 : at - 1);      // into the stage consumed in the last turn
+            if (s < 0) continue;
             const uint2 stage = (plain >> at) & 1 ? make_uint2(kAllRows, 0u) : s_stage[warp][at];
             if (s == 0 || (stage.y & kFirst)) {
                 now = s_pair[warp][at];
@@ -806,8 +837,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
             if (ends || s == my_tiles - 1) {
                 sum_up();
                 if (ends && begun_here) write_out(now.pair);
-                else if (!begun_here) keep_part(0, part0, now);
-                else keep_part(1, reinterpret_cast<float *>(smem + (ring - smem0)), now);     // (nothing is on its way into the ring any more)
+                else keep_part(begun_here, begun_here ? reinterpret_cast<float *>(smem + (ring - smem0)) : part0, now);     // (nothing is on its way into the ring any more)
             }
             at = at + 1 == G::kStages ? 0 : at + 1;
         }
@@ -818,104 +848,115 @@ decode_attn_kernel(const __grid_constant__ Args a) {
     // ---- the block's parts.  A chain is one pair's: a part at a stretch's end (c - 1 is the warp; or, c = 0, of a pair that began before
     // the block, at the first stretch's beginning), then the following warps' parts at their beginnings.
     const int first = s_first[0], last = s_first[NW];      // the block's tiles
+    auto write_joined = [&](int pair, int col, int el, float top, float sum, const float4 &o) {
+        const size_t head = (size_t)pair * a.g + col;
+        const float inv = top == -INFINITY ? 0.f : about_one_over(sum);
+        *reinterpret_cast<uint2 *>(a.out + head * D + el) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+        if (a.lse && el == 0) a.lse[head] = top == -INFINITY ? -INFINITY : (top + lg2(sum)) * 0.6931471805599453f;
+    };
+    // A thread takes four elements of a query; 16 threads side by side (a query's, or half of one's) share out the parts' references and
+    // sums.  Little code, in rolled loops: what runs once costs what it takes to fetch.
+    const int per = a.g * (D / 4), sub16 = lane & 15;
+    auto max16 = [](float x) {
+#pragma unroll
+        for (int o = 8; o > 0; o /= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+        return x;
+    };
+    auto sum16 = [](float x) {
+#pragma unroll
+        for (int o = 8; o > 0; o /= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
+        return x;
+    };
+    auto add = [](float4 &o, const float4 &y, float f) { o.x = fmaf(y.x, f, o.x), o.y = fmaf(y.y, f, o.y), o.z = fmaf(y.z, f, o.z), o.w = fmaf(y.w, f, o.w); };
+    static_assert(NW <= 16, "");
+    const float *const beginnings = reinterpret_cast<const float *>(smem + G::kRing);
+    int turn = 0;                                          // (chains one after the other, to different warps)
+#pragma unroll 1
     for (uint32_t left = __ballot_sync(0xffffffffu, lane <= NW && s_part[max(min(lane, NW) - 1, 0)][lane == 0 ? 0 : 1].tiles >= 0); left; left &= left - 1) {
         const int c = __ffs(left) - 1, w0 = max(c - 1, 0), which = c == 0 ? 0 : 1;
         const Pair pt = s_part[w0][which];
         const int end = pt.begin + pt.tiles;
-        const int n = 1 + __popc(__ballot_sync(0xffffffffu, lane > w0 && lane < NW && s_first[min(lane, NW)] < end));        // warps with a part of it
         const bool here = pt.begin >= first && end <= last;
         if (tid == 0 && !here) s_leaves[pt.begin >= first ? 1 : 0] = c;
-        const size_t slot = 2 * (size_t)blockIdx.x + (pt.begin >= first ? 1 : 0);
-        const size_t head0 = (size_t)(pt.pair / a.H_kv) * a.H_q + pt.pair % a.H_kv * a.g;
-        for (int i = tid; i < a.g * (D / 2); i += NT) {
-            const int col = i / (D / 2), el = i % (D / 2) * 2;
-            const float *src0 = which == 1 ? reinterpret_cast<const float *>(smem + w0 * G::kStages * G::kStageBytes)
-                                           : reinterpret_cast<const float *>(smem + G::kRing) + w0 * G::kPart;
-            float2 ml[NW];                                  // (all loads at once)
-#pragma unroll
-            for (int w = 0; w < NW; ++w) ml[w] = w < n ? s_ml[min(w0 + w, NW - 1)][w ? 0 : which][col] : make_float2(-INFINITY, 0.f);
-            float top = ml[0].x;
-#pragma unroll
-            for (int w = 1; w < NW; ++w) top = fmaxf(top, ml[w].x);
-            const float ref = top == -INFINITY ? 0.f : top;
-            float2 o = *reinterpret_cast<const float2 *>(src0 + col * RP + el);
-            float f = ex2(ml[0].x - ref), sum = ml[0].y * f;
-            o.x *= f, o.y *= f;
-#pragma unroll
-            for (int w = 1; w < NW; ++w)
-                if (w < n) {
-                    const float2 y = *reinterpret_cast<const float2 *>(reinterpret_cast<const float *>(smem + G::kRing) + (w0 + w) * G::kPart + col * RP + el);
-                    f = ex2(ml[w].x - ref);
-                    sum = fmaf(ml[w].y, f, sum);
-                    o.x = fmaf(y.x, f, o.x), o.y = fmaf(y.y, f, o.y);
-                }
+        const bool has = sub16 < NW - w0 && (sub16 == 0 || s_first[w0 + sub16] < end);           // that warp has a part of it
+        const int n = __popc(__ballot_sync(0xffffffffu, has)) / 2;
+#pragma unroll 1
+        for (int i0 = (warp >= turn ? warp - turn : warp - turn + NW) * 32; i0 < per; i0 += NT) {
+            const uint32_t i = i0 + lane, col = i / (D / 4), el = i % (D / 4) * 4;          // (per is a multiple of 16: 16 threads are all there or none)
+            const bool mine = i < (uint32_t)per;
+            const float2 ml = mine && has ? s_ml[w0 + sub16][sub16 ? 0 : which][col] : make_float2(-INFINITY, 0.f);
+            const float top = max16(ml.x), f = ex2(ml.x - (top == -INFINITY ? 0.f : top)), sum = sum16(ml.y * f);
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            const float *y = which == 1 ? reinterpret_cast<const float *>(smem + w0 * G::kStages * G::kStageBytes) : beginnings + w0 * G::kPart;
+#pragma unroll 2
+            for (int w = 0; w < n; ++w) {
+                const float fw = __shfl_sync(0xffffffffu, f, w, 16);
+                if (mine) add(o, *reinterpret_cast<const float4 *>(y + col * RP + el), fw);
+                y = beginnings + (w0 + w + 1) * G::kPart;
+            }
+            if (!mine) continue;
             if (here) {
-                const float inv = top == -INFINITY ? 0.f : 1.f / sum;
-                *reinterpret_cast<uint32_t *>(a.out + (head0 + col) * D + el) = pack_bf16(o.x * inv, o.y * inv);
-                if (a.lse && el == 0) a.lse[head0 + col] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+                write_joined(pt.pair, col, el, top, sum, o);
             } else {
-                __stcg(reinterpret_cast<float2 *>(a.ws_o + (slot * kMaxGroup + col) * D + el), o);
+                const size_t slot = 2 * (size_t)blockIdx.x + (pt.begin >= first ? 1 : 0);
+                __stcg(reinterpret_cast<float4 *>(a.ws_o + (slot * kMaxGroup + col) * D + el), o);
                 if (el == 0) __stcg(a.ws_ml + slot * kMaxGroup + col, make_float2(top, sum));
             }
         }
+        turn = min(turn + (per + 31) / 32, NW) % NW;
     }
     __syncthreads();
     // A pair that leaves the block (two at most: one that began before it, one that goes on behind it) has parts with the blocks b0 .. b1;
     // the last of them to arrive joins them, in their order.
-    if (s_leaves[0] < 0 && s_leaves[1] < 0) return empty_requests<D, NT, T>(a);
-    if (tid < 64 && lane == 0 && s_leaves[warp] >= 0) {
+    const bool leaves = s_leaves[0] >= 0 || s_leaves[1] >= 0;
+    if (leaves && tid < 64 && lane == 0 && s_leaves[warp] >= 0) {
         const int c = s_leaves[warp];
         const Pair pt = s_part[max(c - 1, 0)][c == 0 ? 0 : 1];
-        const int workers = s_shared[0], all = s_shared[1];
-        const int b0 = worker_of(pt.begin, workers, all) / NW, b1 = worker_of(pt.begin + pt.tiles - 1, workers, all) / NW;
+        const Shares shares(s_shared[0], s_shared[1]);
+        const int b0 = pt.begin >= first ? (int)blockIdx.x : shares.of(pt.begin) / NW;
+        const int b1 = pt.begin + pt.tiles <= last ? (int)blockIdx.x : shares.of(pt.begin + pt.tiles - 1) / NW;
         uint32_t before;                               // (back to 0 with the last)
         asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(before) : "l"(a.ws_count + b0), "r"((uint32_t)(b1 - b0)) : "memory");
         s_join[warp][0] = b0;
         s_join[warp][1] = before == (uint32_t)(b1 - b0) ? b1 - b0 + 1 : 0;
     }
-    __syncthreads();
+    if (leaves) __syncthreads();
 #pragma unroll 1
-    for (int which = 0; which < 2; ++which) {
-        const int c = s_leaves[which];
-        if (c < 0) continue;
-        const int b0 = s_join[which][0], n_parts = s_join[which][1], pair = s_part[max(c - 1, 0)][c == 0 ? 0 : 1].pair;
-        if (n_parts == 0) continue;
-        const size_t head0 = (size_t)(pair / a.H_kv) * a.H_q + pair % a.H_kv * a.g;
-        for (int i = tid; i < a.g * (D / 2); i += NT) {
-            const int col = i / (D / 2), el = i % (D / 2) * 2;
-            float top = -INFINITY, sum = 0.f;
-            float2 o = make_float2(0.f, 0.f);
-            constexpr int kInFlight = 20;
-            for (int p0 = 0; p0 < n_parts; p0 += kInFlight) {
-                float2 ml[kInFlight], y[kInFlight];
+    for (int i0 = warp * 32; leaves && i0 < 2 * per; i0 += NT) {             // (both pairs at once)
+        const uint32_t i = i0 + lane, which = i >= (uint32_t)per, it = i - which * per, col = it / (D / 4), el = it % (D / 4) * 4;
+        const int c = i < 2u * per ? s_leaves[which] : -1, n_parts = c < 0 ? 0 : s_join[which][1];
+        const int b0 = s_join[which][0];
+        float top = -INFINITY, sum = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        constexpr int kInFlight = 20;
+#pragma unroll 1
+        for (int p0 = 0; p0 < __reduce_max_sync(0xffffffffu, n_parts); p0 += kInFlight) {
+            // part p's slot is 2 (b0 + p), of the first one more
+            constexpr int kStep = 2 * kMaxGroup;
+            const size_t row0 = (size_t)(b0 + p0) * kStep + col;
+            const int first_too = p0 == 0 ? kMaxGroup : 0;
+            float2 ml[2];
+            float4 y[kInFlight];
 #pragma unroll
-                for (int p = 0; p < kInFlight; ++p)
-                    if (p0 + p < n_parts) {
-                        const size_t from = (2 * (size_t)(b0 + p0 + p) + (p0 + p == 0 ? 1 : 0)) * kMaxGroup + col;
-                        ml[p] = __ldcg(a.ws_ml + from);
-                        y[p] = __ldcg(reinterpret_cast<const float2 *>(a.ws_o + from * D + el));
-                    } else {
-                        ml[p] = make_float2(-INFINITY, 0.f);
-                        y[p] = make_float2(0.f, 0.f);
-                    }
-                float mx = top;
-#pragma unroll
-                for (int p = 0; p < kInFlight; ++p) mx = fmaxf(mx, ml[p].x);
-                const float ref = mx == -INFINITY ? 0.f : mx, f0 = ex2(top - ref);
-                sum *= f0;
-                o.x *= f0, o.y *= f0;
-#pragma unroll
-                for (int p = 0; p < kInFlight; ++p) {
-                    const float f = ex2(ml[p].x - ref);
-                    sum = fmaf(ml[p].y, f, sum);
-                    o.x = fmaf(y[p].x, f, o.x), o.y = fmaf(y[p].y, f, o.y);
-                }
-                top = mx;
+            for (int u = 0; u < 2; ++u) {
+                const int p = sub16 + 16 * u;
+                ml[u] = p < kInFlight && p0 + p < n_parts ? __ldcg(a.ws_ml + row0 + p * kStep + (p == 0 ? first_too : 0)) : make_float2(-INFINITY, 0.f);
             }
-            const float inv = top == -INFINITY ? 0.f : 1.f / sum;
-            *reinterpret_cast<uint32_t *>(a.out + (head0 + col) * D + el) = pack_bf16(o.x * inv, o.y * inv);
-            if (a.lse && el == 0) a.lse[head0 + col] = top == -INFINITY ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+            const float *from = a.ws_o + row0 * D + el;
+#pragma unroll
+            for (int p = 0; p < kInFlight; ++p) {
+                y[p] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (p0 + p < n_parts) y[p] = __ldcg(reinterpret_cast<const float4 *>(p == 0 ? from + first_too * D : from + p * (kStep * D)));
+            }
+            const float mx = fmaxf(top, max16(fmaxf(ml[0].x, ml[1].x))), ref = mx == -INFINITY ? 0.f : mx, f0 = ex2(top - ref);
+            const float f[2] = {ex2(ml[0].x - ref), ex2(ml[1].x - ref)};
+            sum = fmaf(sum, f0, sum16(fmaf(ml[0].y, f[0], ml[1].y * f[1])));
+            o.x *= f0, o.y *= f0, o.z *= f0, o.w *= f0;
+#pragma unroll
+            for (int p = 0; p < kInFlight; ++p) add(o, y[p], __shfl_sync(0xffffffffu, f[p / 16], p % 16, 16));
+            top = mx;
         }
+        if (n_parts > 0) write_joined(s_part[max(c - 1, 0)][c == 0 ? 0 : 1].pair, col, el, top, sum, o);
     }
     empty_requests<D, NT, T>(a);
 }
