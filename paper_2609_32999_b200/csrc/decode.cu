@@ -15,7 +15,7 @@
 // before or goes on behind its stretch is a part; at the end the block joins its warps' parts, and parts of pairs that
 // leave the block go to the workspace, where the last block to arrive joins them, always in the order of the tiles.
 // (Blocks that took pairs in turn, all their warps on one, and met at the end of each: 215 us where 64 requests of 200 to
-// 16 384 tokens, 8 heads in 4 bits, then took 130 us, now 113; a join in a kernel of its own: 4 us more for any batch.)
+// 16 384 tokens, 8 heads in 4 bits, then took 130 us, now 109; a join in a kernel of its own: 4 us more for any batch.)
 // A row that is not visible, past the end or on a page outside the pool is filled with zeros and never read, so what stands
 // there does not matter.
 #include <cmath>
@@ -61,13 +61,13 @@ struct Args {
 // its stretch begins in; the part of the one it ends in goes into the ring.
 template <int D, bool F4, int NQ> struct Geo {
     // (4-bit, 64 requests of up to 16 384 tokens, 8 heads: 12 warps of 168 registers 113 us, with a third stage 112 but a lone request
-    // 12.0 -> 12.5; 16 of 128 115, 14 127.  Two fifths of the instructions spread codes over operands; their pipe is busy 56 % of the time.)
+    // 12.0 -> 12.5; 16 of 128 115, 14 127; later, with the joins in less code, 12 warps 109.  Two fifths of the instructions spread codes over operands; their pipe is busy 56 % of the time.)
     static constexpr int kWarps = F4 && NQ == 1 ? 12 : 8;
     static constexpr int kThreads = 32 * kWarps;
     static constexpr int kTile = F4 ? 32 : 16;                            // keys
     static constexpr int kRow = F4 ? D / 2 : 2 * D;                       // bytes of a row of K or V
     static constexpr int kStageBytes = 2 * kTile * (kRow + (F4 ? 8 : 0));
-    static constexpr int kFew = F4 ? 44 : 56;                             // tiles that a block may have more for whole pairs (see stretch_of)
+    static constexpr int kFew = F4 ? 24 : 30;                             // tiles that a block may have more for whole pairs (see stretch_of)
     static constexpr int kPart = 8 * NQ * (D + 4);                        // floats; rows 4 apart in banks: the lanes of a store spread over all
     static constexpr int kStages = F4 ? (NQ == 1 ? 2 : 4) * (128 / D) : (NQ == 1 ? 3 : 2) * (128 / D);
     static constexpr int kRing = kWarps * kStages * kStageBytes;
@@ -171,9 +171,10 @@ struct Shares {
 // A warp's stretch of the batch's `all` tiles: [first, last), beginning in request r, before which lie `before` tiles.  Every warp sums the
 // batch by itself, a stretch of the requests a lane: no waiting for others, and the lengths are in L1 after the first.
 // As a rule all warps of the grid, `workers` of them, share the tiles evenly.  Where that makes no block's share much larger, blocks
-// share the pairs instead, whole, and a block's warps their tiles: no parts leave a block then, and joining them takes 3 to 5 us.
-// "Much": by more than `few` tiles, by the bound pairs a block x tiles of the longest pair.  (One request of 300 tokens, 8 heads, 9.1 ->
-// 6.0 us, 4-bit 10.9 -> 6.7; 16 of 900 14.3 -> 10.3; alone 1 300 tokens would take 11.5 for 9.8.)
+// share the pairs instead, whole, and a block's warps their tiles: no parts leave a block then, and joining them takes 2 us.
+// "Much": by more than `few` tiles, by the bound pairs a block x tiles of the longest pair.  (8 heads; whole for shared, us: one request
+// of 300 tokens 6.1 for 6.6, of 600 7.6 for 6.7, 8 of 600 7.8 for 8.9, 64 of 300 13.0 for 14.5; 4-bit, one of 300 6.6 for 8.2, of 600
+// 7.7 for 8.3, of 900 9.0 for 8.4, 8 of 600 8.0 for 8.9.)
 struct Stretch { int first, last, all, workers, r, before; };
 template <int T, int NW>
 __device__ __forceinline__ Stretch stretch_of(const Args &a, int few) {
@@ -855,7 +856,9 @@ decode_attn_kernel(const __grid_constant__ Args a) {
         if (a.lse && el == 0) a.lse[head] = top == -INFINITY ? -INFINITY : (top + lg2(sum)) * 0.6931471805599453f;
     };
     // A thread takes four elements of a query; 16 threads side by side (a query's, or half of one's) share out the parts' references and
-    // sums.  Little code, in rolled loops: what runs once costs what it takes to fetch.
+    // sums.  Little code, in rolled loops: what runs once costs what it takes to fetch.  (Written out part by part for every thread, pair
+    // after pair, and with three copies of fetch(), the kernel had 85 KB of code for 49; a lone request of 5 312 tokens took 12.0 us, now
+    // 9.0, 64 of 200 to 16 384 tokens in 4 bits 113, now 109.)
     const int per = a.g * (D / 4), sub16 = lane & 15;
     auto max16 = [](float x) {
 #pragma unroll
