@@ -33,6 +33,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <cmath>
 
 #include "device_mem.cuh"
 #include "launch.h"
@@ -144,7 +145,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
                const AttnWork *__restrict__ work, int n_work, const int32_t *__restrict__ q_pos,
                const int32_t *__restrict__ pages, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse,
                int H_q, int g, int page_size, int num_pool_pages, float scale_log2,
-               float *__restrict__ ws_o, float2 *__restrict__ ws_ml, int *status, int window, int n_sink) {
+               float *__restrict__ ws_o, float2 *__restrict__ ws_ml, int *status, int window, int n_sink, uint32_t sign_s) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     using G = Geo<D>;
@@ -351,7 +352,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant
         // tile 0, warp 10 for tile 1.  Each runs its own tile's chain, so the waits of one overlap
         // the MMAs of the other; a ring slot is free again once both have released it (the warp of a
         // tile that is absent or already finished only releases).
-        constexpr uint32_t idesc_s = K8 ? idesc_e4m3(kRows, kStep) : idesc_bf16(kRows, kStep, false);
+        const uint32_t idesc_s = (K8 ? idesc_e4m3(kRows, kStep) : idesc_bf16(kRows, kStep, false)) | sign_s;
         constexpr uint32_t idesc_o = idesc_bf16(kRows, kD, true);
         const int q = warp - 9;
         const uint32_t qbase = smem_u32(sm + kSmemQ + q * kQTileBytes);
@@ -906,7 +907,9 @@ cudaError_t launch_attn_tc_d(const tessera_plan *pl, void *k_pool, void *v_pool,
     cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<D, kMaxPages, K8, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Geo<D>::kSmemAlloc);
     if (e != cudaSuccess) { *err = "cudaFuncSetAttribute(shared memory)"; return e; }
     const DeviceTables &d = pl->dev;
-    const float scale_log2 = pl->sm_scale * 1.4426950408889634f * qk_scale;
+    // Of a negative scale the sign goes into the product S = (-Q) K^T: masks and maxima then are those of a positive one.
+    const float scale_log2 = std::fabs(pl->sm_scale) * 1.4426950408889634f * qk_scale;
+    const uint32_t sign_s = pl->sm_scale < 0.f ? kIdescNegateA : 0u;
     // A chained grid comes in clusters of two, though the blocks share nothing by themselves: neighbours in the list
     // read the same K/V pages at about the same time, and the two SMs of a TPC fetch a line that both ask for once.
     // An ordinary launch places blocks 2 i and 2 i + 1 that way by itself, a chained one wherever an SM becomes free:
@@ -916,7 +919,7 @@ cudaError_t launch_attn_tc_d(const tessera_plan *pl, void *k_pool, void *v_pool,
     if (chained && grid % 2 != 0 && max_blocks <= 0 && grid < (unsigned)pl->num_sms) ++grid;      // (a block without an item ends at once)
     e = launch_clusters(
         attn_tc_kernel<D, kMaxPages, K8, W>, grid, kThreads, chained && grid % 2 == 0 ? 2 : 1, Geo<D>::kSmemAlloc, st, chained, tq, tk, tv, to, d.tiles, work, (int)n_work, d.q_pos, d.pages,
-        static_cast<__nv_bfloat16 *>(out), lse, Hq, g, ps, pl->num_pool_pages, scale_log2, d.ws_o, d.ws_ml, d.status, pl->window, pl->n_sink);
+        static_cast<__nv_bfloat16 *>(out), lse, Hq, g, ps, pl->num_pool_pages, scale_log2, d.ws_o, d.ws_ml, d.status, pl->window, pl->n_sink, sign_s);
     if (e == cudaSuccess && !pl->combine.empty()) {
         const int c0 = chunk < 0 ? 0 : pl->chunk_combine_off[chunk];
         const int c1 = chunk < 0 ? (int)pl->combine.size() : pl->chunk_combine_off[chunk + 1];

@@ -210,6 +210,9 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, bool b_mn_major)
            ((uint32_t)(M >> 4) << 24);
 }
 
+// Set in an instruction descriptor (kind::f16, kind::f8f6f4): A counts negated.
+constexpr uint32_t kIdescNegateA = 1u << 13;
+
 // Instruction descriptor for kind::f8f6f4: e4m3 x e4m3 -> fp32 (operand format code 0), both operands K-major.
 __host__ __device__ constexpr uint32_t idesc_e4m3(int M, int N) {
     return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
