@@ -530,8 +530,9 @@ decode_attn_kernel(const __grid_constant__ Args a) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int col = column(n, e);
-                    inv[e] = m[n][e] == -INFINITY ? 0.f : about_one_over(l[n][e]);
-                    if (a.lse && quad == 0 && col < a.g && (!FOLD || t < 2)) a.lse[head0 + col] = m[n][e] == -INFINITY ? -INFINITY : (m[n][e] + lg2(l[n][e])) * 0.6931471805599453f;
+                    // (by the sum: the reference stays at -inf where all scores are NaN, too, and NaN is then the result)
+                    inv[e] = l[n][e] == 0.f ? 0.f : about_one_over(l[n][e]);
+                    if (a.lse && quad == 0 && col < a.g && (!FOLD || t < 2)) a.lse[head0 + col] = l[n][e] == 0.f ? -INFINITY : (m[n][e] + lg2(l[n][e])) * 0.6931471805599453f;
                 }
                 if constexpr (F4) {
                     // (accumulators e and e + 2 are neighbouring elements)
@@ -851,9 +852,9 @@ decode_attn_kernel(const __grid_constant__ Args a) {
     const int first = s_first[0], last = s_first[NW];      // the block's tiles
     auto write_joined = [&](int pair, int col, int el, float top, float sum, const float4 &o) {
         const size_t head = (size_t)pair * a.g + col;
-        const float inv = top == -INFINITY ? 0.f : about_one_over(sum);
+        const float inv = sum == 0.f ? 0.f : about_one_over(sum);
         *reinterpret_cast<uint2 *>(a.out + head * D + el) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-        if (a.lse && el == 0) a.lse[head] = top == -INFINITY ? -INFINITY : (top + lg2(sum)) * 0.6931471805599453f;
+        if (a.lse && el == 0) a.lse[head] = sum == 0.f ? -INFINITY : (top + lg2(sum)) * 0.6931471805599453f;
     };
     // A thread takes four elements of a query; 16 threads side by side (a query's, or half of one's) share out the parts' references and
     // sums.  Little code, in rolled loops: what runs once costs what it takes to fetch.  (Written out part by part for every thread, pair
