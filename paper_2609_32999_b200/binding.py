@@ -117,6 +117,13 @@ class TesseraError(RuntimeError):
         self.status = status
 
 
+class ArgumentError(TesseraError, ValueError):
+    """A tensor of the wrong kind, refused before the library is called."""
+
+    def __init__(self, text: str):
+        super().__init__(INVALID_ARG, text)
+
+
 def last_error() -> str:
     buf = ctypes.create_string_buffer(512)
     _lib.tessera_last_error(buf, 512)
@@ -144,6 +151,11 @@ def _dev(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _current_device() -> int:
+    import torch
+    return torch._C._cuda_getDevice()
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
@@ -166,11 +178,22 @@ def _expect(what: str, t, index: int, dtype, shape, rows: bool = False) -> int:
     if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
         return 0
     if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
-        raise ValueError("%s: expected %s of %s on device %d, got %s of %s on device %d"
-                         % (what, tuple(shape), dtype, index, tuple(t.shape), t.dtype, t.get_device()))
+        raise ArgumentError("%s: expected %s of %s on device %d, got %s of %s on device %d"
+                            % (what, tuple(shape), dtype, index, tuple(t.shape), t.dtype, t.get_device()))
     if not (rows and t.stride()[1:] == (shape[2], 1) and t.stride(0) >= shape[1] * shape[2]):
-        raise ValueError("%s: strides %s" % (what, tuple(t.stride())))
+        raise ArgumentError("%s: strides %s" % (what, tuple(t.stride())))
     return t.stride(0)
+
+
+def _expect_pool(what: str, t, index: int, dtype, shape, pinned: bool = False) -> None:
+    """A contiguous pool of at least shape[0] pages on the device or (pinned) in page-locked host memory.  What is None the library
+    refuses by itself."""
+    if t is None or (t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()):
+        return
+    there = t.get_device() == index or (pinned and t.device.type == "cpu" and t.is_pinned())
+    if not (there and t.dtype is dtype and t.dim() == len(shape) and t.shape[0] >= shape[0] and t.shape[1:] == shape[1:] and t.is_contiguous()):
+        raise ArgumentError("%s: expected %s (or more pages) of %s, contiguous, on device %d, got %s of %s on %s"
+                            % (what, tuple(shape), dtype, index, tuple(t.shape), t.dtype, t.device))
 
 
 def _fresh_rows(sh, n: int, index: int, bfloat16, q, q_out, k, v, q_weight, k_weight, eps) -> FreshRows:
@@ -211,6 +234,9 @@ class Plan:
         self._opt = opt
         self._h = _vp()
         self.host_only = host_only
+        self._row = (sh.page_size, sh.num_kv_heads, sh.head_dim)
+        self._pool = (int(w.num_pool_pages),) + self._row
+        self._cache = (desc.retain_pool_pages,) + self._row if desc.retain_pool_pages > 0 else self._pool
         args = (PLAN_HOST_ONLY if host_only else 0, ctypes.byref(self._h), None if host_only else _stream(stream))
         if window == 0 and n_sink == 0:
             st = _lib.tessera_plan_create(ctypes.byref(cfg), ctypes.byref(desc), int(w.num_pool_pages), *args)
@@ -288,9 +314,16 @@ class Plan:
     def extend_write_norm(self, k_pool, v_pool, q, q_out, k_new_raw, v_new, q_weight=None, k_weight=None, eps: float = 1e-6, k_cache=None,
                           v_cache=None, stream=None) -> None:
         """extend_write with per-head norms of q and k before the rotation, q written to q_out (q itself, or another tensor); q, k_new_raw and
-        v_new may be slices [n_q, heads, D] of a fused projection.  q None: keys and values alone."""
+        v_new may be slices [n_q, heads, D] of a fused projection.  q None: keys and values alone.  All tensors live on the plan's device, the
+        current one; cache pools may be page-locked host memory."""
         from torch import bfloat16
-        rows = _fresh_rows(self.shape, int(self.info.n_q), k_new_raw.get_device(), bfloat16, q, q_out, k_new_raw, v_new, q_weight, k_weight, eps)
+        index = -1 if self.host_only else _current_device()            # (the library refuses a current device that is not the plan's)
+        _expect_pool("k_pool", k_pool, index, bfloat16, self._pool)
+        _expect_pool("v_pool", v_pool, index, bfloat16, self._pool)
+        if self.info.retained_tokens > 0:
+            _expect_pool("k_cache", k_cache, index, bfloat16, self._cache, pinned=True)
+            _expect_pool("v_cache", v_cache, index, bfloat16, self._cache, pinned=True)
+        rows = _fresh_rows(self.shape, int(self.info.n_q), index, bfloat16, q, q_out, k_new_raw, v_new, q_weight, k_weight, eps)
         _check(_lib.tessera_extend_write_norm(self._h, _dev(k_pool), _dev(v_pool), ctypes.addressof(rows), _dev(k_cache), _dev(v_cache), _stream(stream)))
 
     def partial_prefill_attn(self, k_pool, v_pool, q, k_new, v_new, out, lse=None, stream=None) -> None:
