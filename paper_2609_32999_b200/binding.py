@@ -236,6 +236,8 @@ class Plan:
         self.host_only = host_only
         self._row = (sh.page_size, sh.num_kv_heads, sh.head_dim)
         self._pool = (int(w.num_pool_pages),) + self._row
+        self._sources = (desc.num_source_pages,) + self._row
+        self._pool4, self._sources4 = pool4_shape(sh, self._pool[0]), pool4_shape(sh, self._sources[0])
         self._cache = (desc.retain_pool_pages,) + self._row if desc.retain_pool_pages > 0 else self._pool
         args = (PLAN_HOST_ONLY if host_only else 0, ctypes.byref(self._h), None if host_only else _stream(stream))
         if window == 0 and n_sink == 0:
@@ -288,15 +290,29 @@ class Plan:
         _check(_lib.tessera_kv_retain_fp8(self._h, _dev(k_src), _dev(v_src), _dev(k_dst8), _dev(v_dst8), k_scale, v_scale,
                                           FUSE_ROPE if fuse_rope else 0, _stream(stream)))
 
+    def _tier4(self, k_src, v_src, source_dtype, sources, k_dst, v_dst, dtype, pool, stream):
+        """Checks the pools of a 4-bit tier call; returns the stream's handle.  (A plan that serves no such call the library refuses.)"""
+        if self.host_only or self._sources[0] <= 0:
+            return None
+        index = _current_device()                                      # (the library refuses a current device that is not the plan's)
+        _expect_pool("k source", k_src, index, source_dtype, sources, pinned=True)
+        _expect_pool("v source", v_src, index, source_dtype, sources, pinned=True)
+        _expect_pool("k destination", k_dst, index, dtype, pool, pinned=True)
+        _expect_pool("v destination", v_dst, index, dtype, pool, pinned=True)
+        return _stream(stream)
+
     def kv_retain_kv4(self, k_src, v_src, k_dst4, v_dst4, fuse_rope: bool = True, stream=None) -> None:
-        """16-bit source pools -> 4-bit pools (pool4_shape); the plan's destination pages index the 4-bit pools."""
-        _check(_lib.tessera_kv_retain_kv4(self._h, _dev(k_src), _dev(v_src), _dev(k_dst4), _dev(v_dst4), FUSE_ROPE if fuse_rope else 0,
-                                          _stream(stream)))
+        """16-bit source pools -> 4-bit pools (pool4_shape); the plan's destination pages index the 4-bit pools.  Pools live on the plan's device,
+        the current one, or in page-locked host memory, and may have more pages than the plan counts."""
+        import torch
+        st = self._tier4(k_src, v_src, torch.bfloat16, self._sources, k_dst4, v_dst4, torch.uint8, self._pool4, stream)
+        _check(_lib.tessera_kv_retain_kv4(self._h, _dev(k_src), _dev(v_src), _dev(k_dst4), _dev(v_dst4), FUSE_ROPE if fuse_rope else 0, st))
 
     def kv_compose_from_kv4(self, k_src4, v_src4, k_pool, v_pool, fuse_rope: bool = True, stream=None) -> None:
-        """Sources in 4-bit pools (pool4_shape), destinations in the 16-bit pools, keys rotated on the way."""
-        _check(_lib.tessera_kv_compose_from_kv4(self._h, _dev(k_src4), _dev(v_src4), _dev(k_pool), _dev(v_pool), FUSE_ROPE if fuse_rope else 0,
-                                                _stream(stream)))
+        """Sources in 4-bit pools (pool4_shape), destinations in the 16-bit pools, keys rotated on the way.  Pools as for kv_retain_kv4."""
+        import torch
+        st = self._tier4(k_src4, v_src4, torch.uint8, self._sources4, k_pool, v_pool, torch.bfloat16, self._pool, stream)
+        _check(_lib.tessera_kv_compose_from_kv4(self._h, _dev(k_src4), _dev(v_src4), _dev(k_pool), _dev(v_pool), FUSE_ROPE if fuse_rope else 0, st))
 
     def rope_shift(self, k_pool, stream=None) -> None:
         _check(_lib.tessera_rope_shift(self._h, _dev(k_pool), _stream(stream)))

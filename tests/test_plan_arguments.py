@@ -83,3 +83,60 @@ def test_normalising_write_pools_on_another_device(device_plan):
     with pytest.raises(ValueError) as e:
         plan.extend_write_norm(**a)
     assert "k_pool" in str(e.value) and not calls
+
+
+def tier_workload():
+    """Units of 20 and 5 tokens out of a source pool of 9 pages into a pool of 6."""
+    i = lambda *x: np.array(x, np.int32)
+    return wl.Workload("tier", SHAPE, i(20, 5), i(0, 1, 2), i(20, 5), i(0, 0), i(1, 1), i(0, 0), i(0, 2, 3), i(8, 1, 4), i(0, 0, 0), i(), i(5, 0, 2), 6,
+                       num_source_pages=9)
+
+
+def four_bit(pages, shape=SHAPE):
+    return torch.zeros(tb.pool4_shape(shape, pages), dtype=torch.uint8)
+
+
+WIDE = wl.ModelShape(8, 2, 128, 32, 1e4)
+
+
+@pytest.mark.parametrize("k_src,v_src,k_dst,v_dst", [
+    (four_bit(6), four_bit(6), bf16(9, 16, 2, 128), bf16(9, 16, 2, 128)),                     # source and destination swapped
+    (bf16(8, 16, 2, 128), bf16(9, 16, 2, 128), four_bit(6), four_bit(6)),                     # a source page too few
+    (bf16(9, 16, 2, 128), bf16(9, 16, 2, 128), four_bit(6), four_bit(5)),                     # a destination page too few
+    (bf16(9, 16, 2, 128), bf16(9, 16, 2, 128), four_bit(6, WIDE), four_bit(6, WIDE)),         # another page size
+    (bf16(9, 16, 2, 128), bf16(9, 16, 2, 64), four_bit(6), four_bit(6)),                      # another head_dim
+    (bf16(9, 16, 2, 128), bf16(9, 16, 2, 128).float(), four_bit(6), four_bit(6)),
+    (bf16(9, 16, 2, 128), bf16(9, 16, 2, 128), four_bit(6), four_bit(12)[::2]),               # pages apart
+    (bf16(9, 16, 2, 128), bf16(9, 16, 2, 128), bf16(6, 16, 2, 128), four_bit(6))])
+def test_store_pools(device_plan, k_src, v_src, k_dst, v_dst):
+    plan, calls = device_plan(tier_workload(), -1)
+    with pytest.raises(ValueError) as e:
+        plan.kv_retain_kv4(k_src, v_src, k_dst, v_dst)
+    assert isinstance(e.value, tb.TesseraError) and e.value.status == tb.INVALID_ARG and not calls
+    plan.kv_retain_kv4(bf16(9, 16, 2, 128), bf16(10, 16, 2, 128), four_bit(6), four_bit(99))
+    assert calls == ["tessera_kv_retain_kv4"]
+
+
+@pytest.mark.parametrize("k_src,v_src,k_dst,v_dst", [
+    (bf16(6, 16, 2, 128), bf16(6, 16, 2, 128), four_bit(9), four_bit(9)),
+    (four_bit(9), four_bit(8), bf16(6, 16, 2, 128), bf16(6, 16, 2, 128)),
+    (four_bit(9), four_bit(9), bf16(5, 16, 2, 128), bf16(6, 16, 2, 128)),
+    (four_bit(9, WIDE), four_bit(9), bf16(6, 16, 2, 128), bf16(6, 16, 2, 128)),
+    (four_bit(9), four_bit(9), bf16(6, 2, 16, 128), bf16(6, 16, 2, 128)),
+    (four_bit(9), four_bit(9), bf16(6, 16, 2, 128).half(), bf16(6, 16, 2, 128))])
+def test_load_pools(device_plan, k_src, v_src, k_dst, v_dst):
+    plan, calls = device_plan(tier_workload(), -1)
+    with pytest.raises(ValueError):
+        plan.kv_compose_from_kv4(k_src, v_src, k_dst, v_dst)
+    assert not calls
+    plan.kv_compose_from_kv4(four_bit(9), four_bit(9), bf16(6, 16, 2, 128), bf16(7, 16, 2, 128))
+    assert calls == ["tessera_kv_compose_from_kv4"]
+
+
+def test_tier_pools_in_plain_host_memory(device_plan):
+    plan, calls = device_plan(tier_workload(), 0)
+    with pytest.raises(ValueError):
+        plan.kv_retain_kv4(bf16(9, 16, 2, 128), bf16(9, 16, 2, 128), four_bit(6), four_bit(6))
+    with pytest.raises(ValueError):
+        plan.kv_compose_from_kv4(four_bit(9), four_bit(9), bf16(6, 16, 2, 128), bf16(6, 16, 2, 128))
+    assert not calls
