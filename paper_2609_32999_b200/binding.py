@@ -166,6 +166,16 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream or None
 
 
+def _frequencies(sh, inv_freq) -> Optional[np.ndarray]:
+    """Rotary frequencies as the library reads them: head_dim / 2 numbers."""
+    if inv_freq is None:
+        return None
+    inv = np.ascontiguousarray(inv_freq, dtype=np.float64)
+    if inv.size < sh.head_dim // 2:
+        raise ArgumentError("inv_freq: %d numbers, a head_dim of %d takes %d" % (inv.size, sh.head_dim, sh.head_dim // 2))
+    return inv
+
+
 def _model_cfg(sh, inv: Optional[np.ndarray]) -> ModelCfg:
     return ModelCfg(sh.num_q_heads, sh.num_kv_heads, sh.head_dim, sh.page_size, float(sh.rope_theta),
                     None if inv is None else inv.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
@@ -222,7 +232,7 @@ class Plan:
                        "unit_target_pos", "unit_page_off", "unit_pages", "recompute_off", "recompute_pos",
                        "free_pages")]
         a = self._keep
-        self._inv = None if inv_freq is None else np.ascontiguousarray(inv_freq, dtype=np.float64)
+        self._inv = _frequencies(sh, inv_freq)
         cfg = _model_cfg(sh, self._inv)
         self.shape = sh
         opt = [None if getattr(w, f, None) is None else _arr(getattr(w, f))
@@ -403,6 +413,9 @@ class Decode:
 
     def __init__(self, shape, block_table, seq_lens, num_pool_pages: int, window: int = 0, n_sink: int = 0, inv_freq=None, workspace=None):
         import torch
+        # (the frequencies here, once: 64 powers in every call's host time otherwise)
+        d = shape.head_dim
+        self._inv = _frequencies(shape, [float(shape.rope_theta) ** (-2.0 * m / d) for m in range(d // 2)] if inv_freq is None else inv_freq)
         if block_table.device.type != "cuda" or block_table.dim() != 2:
             raise ValueError("block_table: a [batch, max_pages] tensor on a CUDA device")
         self.shape, self.batch, self.device = shape, int(seq_lens.shape[0]), block_table.device
@@ -411,9 +424,6 @@ class Decode:
         self._bf16, self._f32, self._u8 = torch.bfloat16, torch.float32, torch.uint8
         _expect("block_table", block_table, self._index, torch.int32, (self.batch, int(block_table.shape[1])))
         _expect("seq_lens", seq_lens, self._index, torch.int32, (self.batch,))
-        # (the frequencies here, once: 64 powers in every call's host time otherwise)
-        d = shape.head_dim
-        self._inv = np.ascontiguousarray([float(shape.rope_theta) ** (-2.0 * m / d) for m in range(d // 2)] if inv_freq is None else inv_freq, dtype=np.float64)
         self._cfg = _model_cfg(shape, self._inv)
         self.block_table, self.seq_lens, self.num_pool_pages = block_table, seq_lens, int(num_pool_pages)
         self._desc = DecodeDesc(self.batch, int(block_table.shape[1]), _dev(block_table), _dev(seq_lens), self.num_pool_pages, int(window), int(n_sink))
@@ -490,10 +500,8 @@ def rope_shift_static(shape, k_pool, slots, slot_shift, shifts, stream=None, inv
     """tessera_rope_shift_static: rotate the listed pool slots in place without any device
     allocation.  `slots` / `slot_shift` are int32 device tensors, `shifts` a host int32 sequence;
     `num_pool_slots` (default: every row of k_pool) bounds the slot ids the kernel accepts."""
-    inv = None if inv_freq is None else np.ascontiguousarray(inv_freq, dtype=np.float64)
-    cfg = ModelCfg(shape.num_q_heads, shape.num_kv_heads, shape.head_dim, shape.page_size, float(shape.rope_theta),
-                   None if inv is None else inv.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
-                   int(shape.rope_pairing), float(shape.sm_scale))
+    inv = _frequencies(shape, inv_freq)
+    cfg = _model_cfg(shape, inv)
     sh = _arr(shifts)
     if num_pool_slots is None:
         num_pool_slots = int(k_pool.shape[0]) * int(k_pool.shape[1])
