@@ -996,6 +996,7 @@ int32_t decode_attn(const tessera_model_cfg *cfg, const tessera_decode_desc *d, 
                     float *lse, void *workspace, int64_t bytes, void *stream) {
     std::string err;
     if (int32_t rc = check_decode(cfg, d, &err)) return api_set_error(rc, err);
+    if (!std::isfinite(cfg->sm_scale)) return api_set_error(TESSERA_INVALID_ARG, "sm_scale must be finite");
     if (d->batch == 0) return TESSERA_OK;
     if (!k_pool || !v_pool || misaligned(k_pool) || misaligned(v_pool))
         return api_set_error(TESSERA_INVALID_ARG, "k_pool / v_pool must be non-null and 16-byte aligned");

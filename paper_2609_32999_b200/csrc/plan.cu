@@ -55,6 +55,7 @@ int32_t build_plan_host(const tessera_model_cfg *cfg, const tessera_compose_desc
     if (cfg->rope_pairing != 0 && cfg->rope_pairing != 1)
         return fail(TESSERA_UNSUPPORTED_SHAPE, "rope_pairing: 0 (half-split pairs) or 1 (interleaved pairs)");
     if (!cfg->inv_freq && !(cfg->rope_theta > 0.0)) return fail(TESSERA_INVALID_ARG, "rope_theta must be positive");
+    if (!std::isfinite(cfg->sm_scale)) return fail(TESSERA_INVALID_ARG, "sm_scale must be finite");
     if ((int64_t)num_pool_pages * B > (int64_t)INT32_MAX)
         return fail(TESSERA_UNSUPPORTED_SHAPE, "pool has more than 2^31 slots");
 
