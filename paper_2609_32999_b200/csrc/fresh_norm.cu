@@ -302,7 +302,8 @@ int32_t check_decode(const tessera_model_cfg *cfg, const tessera_decode_desc *d,
     if (d->batch > 0 && (!d->seq_len || (!d->block_table && d->max_pages > 0))) return fail(TESSERA_INVALID_ARG, "null seq_len or block_table");
     if ((int64_t)d->num_pool_pages * B > INT32_MAX) return fail(TESSERA_UNSUPPORTED_SHAPE, "pool has more than 2^31 slots");
     if ((int64_t)d->max_pages * B > (1 << 30)) return fail(TESSERA_UNSUPPORTED_SHAPE, "a block table of more than 2^30 tokens a request");
-    if (((int64_t)d->max_pages * B / kDecodeUnit + 1) * d->batch * H > INT32_MAX) return fail(TESSERA_UNSUPPORTED_SHAPE, "block tables of more than 2^31 tiles of 16 keys");
+    // (tiles a request, divided out: the product of all three passes 64 bits)
+    if (d->batch > 0 && (int64_t)d->max_pages * B / kDecodeUnit + 1 > INT32_MAX / ((int64_t)d->batch * H)) return fail(TESSERA_UNSUPPORTED_SHAPE, "block tables of more than 2^31 tiles of 16 keys");
     return TESSERA_OK;
 }
 
