@@ -46,8 +46,8 @@ __device__ __forceinline__ void norm_chunks(float (&lo)[8], float (&hi)[8], cons
     for (int i = 0; i < 8; ++i) ss = fmaf(lo[i], lo[i], fmaf(hi[i], hi[i], ss));
     const float r = rsqrtf(HeadLanes<D>::sum(ss) * (1.f / D) + eps);
     float wl[8], wh[8];
-    unpack_bf16x8(__ldg(w + c), wl);
-    unpack_bf16x8(__ldg(w + c + D / 16), wh);
+    unpack_bf16x8(ldg_plain(w + c), wl);
+    unpack_bf16x8(ldg_plain(w + c + D / 16), wh);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         lo[i] = lo[i] * r * wl[i];
