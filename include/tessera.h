@@ -331,7 +331,8 @@ typedef struct tessera_fresh_rows {
 /*
  * tessera_extend_write for layers that NORMALISE queries and keys per head before the rotation (the paper's models do not
  * all): every head x of q and k becomes R(p) (w x / sqrt(mean x^2 + eps)), in fp32 with one round-to-nearest-even to bf16 at
- * the end (angle, cosine and sine in fp64).  Values are bit copies.  q goes to q_out, k and v to the rows' destination slots;
+ * the end (angle, cosine and sine in fp64; the squares are summed in fp32, so heads with elements from 2^60 on come out as 0, as
+ * infinities or NaN those whose mean square underflows with eps = 0).  Values are bit copies.  q goes to q_out, k and v to the rows' destination slots;
  * of captured units (desc.unit_retain_page_off) the normalised, un-rotated key, rounded to bf16, and the value go to the cache
  * pages: what a later plan reuses with unit_cached_stride = 0.  With both weights NULL it differs from
  * tessera_extend_write in where q goes.  One kernel; nothing is allocated.  Errors: TESSERA_INVALID_ARG.
@@ -369,12 +370,15 @@ TESSERA_API int32_t tessera_decode_write_kv4(const tessera_model_cfg *cfg, const
 
 /*
  * Attention of one query token a request over its pages:
- *   out[r][h] = softmax(sm_scale * q[r][h] . K[visible][h/g]) . V[visible][h/g];  fp32 scores, sums and accumulators.
+ *   out[r][h] = softmax(sm_scale * q[r][h] . K[visible][h/g]) . V[visible][h/g];  fp32 scores, sums and accumulators.  What the
+ *   tensor cores multiply values by is rounded to bf16: the weights, as in the prefill calls (_kv4: weight times the value's scale).
+ *   _kv4 takes q in fp16, scaled by a power of two for each head: exact but for elements below 2^-26 of the head's greatest.
  *   q, out: device [batch][H_q][D] bf16, q rotated; lse: device [batch][H_q] fp32, natural log, nullable.
  * A request without a token (or none of whose visible keys has a page in the pool) gets out = 0 and lse = -inf.  Keys on
  * pages outside the pool count as not visible; a length above max_pages * page_size counts as that.  Rows that are not
- * visible are not read.  Results do not depend on the timing of the run.  Weights of at most 2^8 times values are summed in fp32 and
- * divided at the end: results are infinite where keys x 2^8 x value reaches 2^128.
+ * visible are not read.  A row with a NaN among its scores gets NaN in out and lse.  Results do not depend on the timing of the run.
+ * Weights of at most 2^8 times values are summed in fp32 and divided at the end: results are infinite where keys x 2^8 x value reaches
+ * 2^128.  _kv4: |q| and sm_scale x |q| have to stay below 2^100 (the unit of a score's sum is a number of its own there).
  *   workspace: device, tessera_decode_workspace_bytes (a function of head_dim and of the current device), 16-byte aligned.  It must
  *   be all zeros before its first use; every call leaves it ready for the next (captured ones too), and in between it must not be
  *   written.  Calls that may overlap on the GPU - two streams, two graphs - need one each.

@@ -7,7 +7,7 @@
 // of a KV head are the narrow side of mma.sync m16n8k16: keys are the 16 rows, queries the 8 (or twice 8) columns, so a
 // score tile is S^T = K Q^T and the output O^T += V^T P^T.  (tcgen05 wants 128 rows of queries; there are at most 16.)
 //
-// Work: the visible keys of every (request, KV head), a pair, are cut into tiles of 16; the tiles of the whole batch, in order, are
+// Work: the visible keys of every (request, KV head), a pair, are cut into tiles of 16, in 4 bits of 32; the tiles of the whole batch, in order, are
 // shared out evenly to the warps of one thread block an SM, whatever the lengths.  Which they are only the device knows (lengths
 // are device data, so that a captured step can be replayed as they grow): every block sums the requests' tiles itself.  A warp
 // goes through its stretch, pair after pair, by itself: it fills a ring of stages with cp.async, the next pair's tiles already on
@@ -15,7 +15,7 @@
 // before or goes on behind its stretch is a part; at the end the block joins its warps' parts, and parts of pairs that
 // leave the block go to the workspace, where the last block to arrive joins them, always in the order of the tiles.
 // (Blocks that took pairs in turn, all their warps on one, and met at the end of each: 215 us where 64 requests of 200 to
-// 16 384 tokens, 8 heads in 4 bits, then took 130 us, now 109; a join in a kernel of its own: 4 us more for any batch.)
+// 16 384 tokens, 8 heads in 4 bits, then took 130 us, now 109 to 124 (boxes); a join in a kernel of its own: 4 us more for any batch.)
 // A row that is not visible, past the end or on a page outside the pool is filled with zeros and never read, so what stands
 // there does not matter.
 #include <cmath>
@@ -61,7 +61,8 @@ struct Args {
 // its stretch begins in; the part of the one it ends in goes into the ring.
 template <int D, bool F4, int NQ> struct Geo {
     // (4-bit, 64 requests of up to 16 384 tokens, 8 heads: 12 warps of 168 registers 113 us, with a third stage 112 but a lone request
-    // 12.0 -> 12.5; 16 of 128 115, 14 127; later, with the joins in less code, 12 warps 109.  Two fifths of the instructions spread codes over operands; their pipe is busy 56 % of the time.)
+    // 12.0 -> 12.5; 16 of 128 115, 14 127; later, with the joins in less code, 12 warps 109 on that box, up to 124 on others.
+    // Not folded: 5 queries a KV head 134, 8 137, 16, in 8 warps of 254 registers, 202; head_dim 64, half the bytes: 4 queries 83, 8 95, 16 154.  Two fifths of the instructions spread codes over operands; their pipe is busy 56 % of the time.)
     static constexpr int kWarps = F4 && NQ == 1 ? 12 : 8;
     static constexpr int kThreads = 32 * kWarps;
     static constexpr int kTile = F4 ? 32 : 16;                            // keys
@@ -859,7 +860,7 @@ decode_attn_kernel(const __grid_constant__ Args a) {
     // A thread takes four elements of a query; 16 threads side by side (a query's, or half of one's) share out the parts' references and
     // sums.  Little code, in rolled loops: what runs once costs what it takes to fetch.  (Written out part by part for every thread, pair
     // after pair, and with three copies of fetch(), the kernel had 85 KB of code for 49; a lone request of 5 312 tokens took 12.0 us, now
-    // 9.0, 64 of 200 to 16 384 tokens in 4 bits 113, now 109.)
+    // 9.0, 64 of 200 to 16 384 tokens in 4 bits 113, then 109.)
     const int per = a.g * (D / 4), sub16 = lane & 15;
     auto max16 = [](float x) {
 #pragma unroll

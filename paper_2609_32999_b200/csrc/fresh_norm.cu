@@ -6,9 +6,9 @@
 //
 // A thread holds 8 elements of a head and the 8 that lie D/2 later, so rotary pairs need no exchange and the sum of squares
 // is three shuffles (two at head_dim 64) among the head's neighbouring threads.  HBM-bound: every row is read and written once.
-// 59 816 rows of 64 + 2 x 8 heads (2.45 GB): 409 us = 5 990 GB/s, 92 % of a copy, with two tasks in flight a thread and three blocks
-// an SM; four tasks and two blocks 450, two and four 408 with spills, more blocks 770 to 950.  A decode step's write is latency: 2.4 us
-// for 8 requests.
+// 59 816 rows of 64 + 2 x 8 heads (2.45 GB): 409 to 431 us (boxes) = 5 990 to 5 680 GB/s, 92 to 87 % of a copy, with two tasks in flight
+// a thread and three blocks an SM (on the box of the 409 four tasks and two blocks took 450, two and four 408 with spills, more blocks
+// 770 to 950).  A decode step's write is latency: 2.4 us for 8 requests.
 #include <cmath>
 #include <cstring>
 #include <string>

@@ -5,9 +5,10 @@
 //   expand : 4-bit pages -> the request's 16-bit pages (keys rotated on the way)
 // A task is a pair-chunk of a row: a thread holds bytes 8 c .. 8 c + 7 of the codes, i.e. elements 8 c .. and their partners
 // D / 2 later, on the 4-bit side one 8-byte access.
-// 73 268 rows of 8 heads of 128 (384 MB read and written a direction, 59 us at the rate of a copy): retain 68 us, whose extremes,
-// quotients and roundings fill 72 % of the issue slots; expand 72 us, waiting for its loads (slots, then codes).  Four blocks an SM
-// with two heads under way a thread; three with four heads 75 us, four with one 89 (expand).
+// 73 268 rows of 8 heads of 128 (384 MB read and written a direction, 59 us at the rate of a copy): retain 68 to 77 us, whose extremes,
+// quotients and roundings fill 72 % of the issue slots, 81 to 89 with keys rotated (see kAhead); expand 72, waiting for its loads (slots, then
+// codes), 68 without rotation.  Four blocks an SM with two heads under way a thread; three with four heads 75 us, four with one 89 (expand).
+// At 64 registers expand with rotation spills 12 bytes, retain with interleaved pairs 4.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -71,8 +72,8 @@ kv4_kernel(const uint8_t *__restrict__ k_src, const uint8_t *__restrict__ v_src,
     if constexpr (TO_4BIT) {
         const uint4 *k = reinterpret_cast<const uint4 *>(k_src) + o16, *v = reinterpret_cast<const uint4 *>(v_src) + o16;
         uint8_t *kd = k_dst + oc, *vd = v_dst + oc, *kn = k_dst + on, *vn = v_dst + on;
-        // The next head is on its way while one is worked on, but for keys that are rotated as well (72 000 rows: 79.5 -> 74.8 us,
-        // rotated 90.7 -> 93.8, for want of registers).
+        // The next head is on its way while one is worked on, but for keys that are rotated as well (72 000 rows, with the quotients one at a
+        // time as they then were: 79.5 -> 74.8 us, rotated 90.7 -> 93.8, for want of registers).
         constexpr bool kAhead = !ROTATE;
         uint4 klo, khi, vlo, vhi, next[4];
         auto load = [&](uint4 &a, uint4 &b, uint4 &x, uint4 &y) { a = ldg_stream(k), b = ldg_stream(k + HALF), x = ldg_stream(v), y = ldg_stream(v + HALF); };
